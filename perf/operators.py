@@ -1,0 +1,658 @@
+"""The operators of a policy step over groups of answers, and what they return.
+
+One sequence-parallel rank that trains on groups of answers to one prompt runs
+
+  front    the split of its projection: norms of every query and key head, the
+           rotation by position, and the layout of the all-to-all, in one pass;
+           its backward takes the gradients as the reverse all-to-all leaves them
+  prefix   attention of packed groups [prompt | answer | answer | ...]: an answer
+           sees its prompt and itself, and the prompt is there once
+  policy   the clipped policy loss with a KL term to a reference model and an
+           entropy term, from the logits, and its gradient to the logits
+
+Each has a forward and a backward.  `listed()` names two cases of each of the six;
+`draw()` gives further ones over the same ranges.  Where `own` is false, `run`
+computes them in elementary torch operations in 32 bits (angles in 64).
+"""
+from __future__ import annotations
+
+import math
+
+import numpy as np
+import torch
+
+own = False
+DEV = "cuda"
+EPS = 1e-6          # of the norms
+THETA = 1000000.0   # base of the rotation's frequencies
+
+
+# ---------------------------------------------------------------- the cases
+def listed():
+    return [
+        # the shortest slices in use: 7 heads over two ranks (a dummy slot), latency
+        dict(name="front_fwd_512_d64", kind="front", dir="fwd", T=512, hs=7, hkv=7, sp=2, D=64, rot=64, pairs="halves",
+             norm=True, base=0),
+        # one of eight ranks of a 32768-token batch, 28 query / 4 KV heads
+        dict(name="front_fwd_4k", kind="front", dir="fwd", T=4096, hs=28, hkv=4, sp=8, D=128, rot=128, pairs="halves",
+             norm=True, base=28672),
+        dict(name="front_bwd_4k", kind="front", dir="bwd", T=4096, hs=28, hkv=4, sp=8, D=128, rot=128, pairs="halves",
+             norm=True, base=28672),
+        # one of sixteen ranks of a long context, 40 / 8 heads, an odd slice, far positions
+        dict(name="front_bwd_8191", kind="front", dir="bwd", T=8191, hs=40, hkv=8, sp=16, D=128, rot=128, pairs="halves",
+             norm=True, base=122865),
+        # short answers to a short prompt, 3 real heads and a dummy one
+        dict(name="prefix_fwd_short_d64", kind="prefix", dir="fwd", groups=2, prompt=300, answers=4, answer=90, hq=3, hkv=3,
+             dummies=1, D=64, layout=1),
+        # eight answers to a long document: one Ulysses rank of a 28 / 4 head model
+        dict(name="prefix_fwd_16k", kind="prefix", dir="fwd", groups=1, prompt=16384, answers=8, answer=900, hq=4, hkv=1,
+             dummies=0, D=128, layout=2),
+        # a packed batch of groups, odd lengths
+        dict(name="prefix_bwd_groups", kind="prefix", dir="bwd", groups=4, prompt=1500, answers=8, answer=420, hq=4, hkv=1,
+             dummies=0, D=128, layout=3),
+        # sixteen answers to a prompt of 8192, with gradients
+        dict(name="prefix_bwd_8k", kind="prefix", dir="bwd", groups=1, prompt=8192, answers=16, answer=600, hq=4, hkv=1,
+             dummies=0, D=128, layout=4),
+        # a rank with few tokens: a row of the vocabulary is all the work there is
+        dict(name="policy_fwd_48", kind="policy", dir="fwd", T=48, V=152064, seqs=2, answer=0.9, kl=0.04, ent=0.0,
+             per_token=False),
+        # a rank's slice, prompts left out of the loss
+        dict(name="policy_fwd_4k", kind="policy", dir="fwd", T=4096, V=152064, seqs=16, answer=0.7, kl=0.04, ent=0.001,
+             per_token=False),
+        dict(name="policy_bwd_150", kind="policy", dir="bwd", T=150, V=152064, seqs=3, answer=0.9, kl=0.04, ent=0.0,
+             per_token=True),
+        dict(name="policy_bwd_4k", kind="policy", dir="bwd", T=4096, V=152064, seqs=16, answer=0.7, kl=0.04, ent=0.001,
+             per_token=False),
+    ]
+
+
+def _log(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def draw(rng):
+    kind, way = rng.choice(["front", "prefix", "policy"]), rng.choice(["fwd", "bwd"])
+    if kind == "front":
+        hs, hkv, n = rng.choice([(7, 7, 2), (28, 4, 8), (40, 8, 16), (14, 2, 4), (28, 4, 1)])
+        D = rng.choice([64, 128, 128])
+        return dict(kind=kind, dir=way, T=_log(rng, 100, 8191), hs=hs, hkv=hkv, sp=n, D=D, rot=rng.choice([D, D, D // 2]),
+                    pairs=rng.choice(["halves", "halves", "neighbours"]), norm=rng.random() < 0.7,
+                    base=rng.randrange(0, 130000))
+    if kind == "prefix":
+        hkv = rng.choice([1, 1, 2])
+        hq = hkv * rng.choice([1, 4, 7] if hkv == 1 else [1, 2])
+        dummies = rng.choice([0, 1]) if hq == hkv else 0
+        groups, answers = rng.choice([1, 1, 2, 3]), rng.randrange(2, 17)
+        prompt, answer = _log(rng, 60, 5000 // groups), _log(rng, 2, 4000 // (groups * answers) + 30)
+        return dict(kind=kind, dir=way, groups=groups, prompt=prompt, answers=answers, answer=answer, hq=hq, hkv=hkv,
+                    dummies=dummies, D=rng.choice([64, 128, 128]), layout=rng.randrange(1000))
+    return dict(kind="policy", dir=way, T=_log(rng, 16, 4000), V=8 * _log(rng, 4000, 19008), seqs=rng.randrange(1, 17),
+                answer=rng.uniform(0.4, 1.0), kl=rng.choice([0.0, 0.04, 0.2]), ent=rng.choice([0.0, 0.001, 0.01]),
+                per_token=rng.random() < 0.5)
+
+
+# ------------------------------------------------------------- descriptions
+def _padded(hs, n):
+    return -(-hs // n) * n
+
+
+def _head_maps(case):
+    """Slot j * H_loc + h of the packed query (key) heads: the head that rank j
+    gets there, or -1.  Query heads are dealt out in order, dummies last; a
+    rank gets the KV heads that its query heads read (MHA: dealt like them)."""
+    hs, hkv, n = case["hs"], case["hkv"], case["sp"]
+    loc = _padded(hs, n) // n
+    qm = np.arange(loc * n)
+    qm[qm >= hs] = -1
+    if hs == hkv:
+        return qm.astype(np.int32), qm.astype(np.int32)
+    g = hs // hkv
+    per = [sorted({h // g for h in range(j * loc, min((j + 1) * loc, hs))}) for j in range(n)]
+    km = np.full((n, max(len(p) for p in per)), -1, np.int32)
+    for j, p in enumerate(per):
+        km[j, :len(p)] = p
+    return qm.astype(np.int32), km.reshape(-1)
+
+
+def _freqs(case):
+    return THETA ** (-2.0 * np.arange(case["rot"] // 2) / case["rot"])
+
+
+def _groups(case):
+    """Segment lengths [prompt, answers...] of every group, and each segment's
+    prompt (-1: a prompt)."""
+    rng = np.random.default_rng(case["layout"])
+
+    def near(median, sigma):
+        return int(np.clip(np.rint(median * math.exp(sigma * rng.standard_normal())), 1, 2 * median + 1))
+    lens, pre = [], []
+    for _ in range(case["groups"]):
+        at = len(lens)
+        lens.append(near(case["prompt"], 0.1))
+        pre.append(-1)
+        for _ in range(case["answers"]):
+            lens.append(near(case["answer"], 0.5))
+            pre.append(at)
+    return np.array(lens), np.array(pre, np.int32)
+
+
+def _attn(case):
+    """Heads, segments and positions of a prefix case."""
+    lens, pre = _groups(case)
+    cu = np.concatenate([[0], np.cumsum(lens)]).astype(np.int32)
+    first = np.where(pre < 0, 0, lens[pre])  # an answer's positions go on where its prompt ends
+    pos = np.concatenate([f + np.arange(n) for f, n in zip(first, lens)]).astype(np.int32)
+    real, H, hkv = case["hq"], case["hq"] + case["dummies"], case["hkv"]
+    if case["dummies"]:  # the last of two ranks
+        heads = dict(H_loc=H, head_offset=H, num_real_heads=H + real, num_padded_heads=2 * H, gqa_group=1, Hkv_loc=H,
+                     kv_head_offset=H)
+        return dict(T=int(cu[-1]), D=case["D"], H=H, real=real, Hkv=H, kv=list(range(real)), heads=heads, cu=cu, pos=pos,
+                    pre=pre, lens=lens)
+    heads = dict(H_loc=H, head_offset=0, num_real_heads=H, num_padded_heads=H, gqa_group=H // hkv, Hkv_loc=hkv,
+                 kv_head_offset=0)
+    return dict(T=int(cu[-1]), D=case["D"], H=H, real=H, Hkv=hkv, kv=[h // (H // hkv) for h in range(H)], heads=heads,
+                cu=cu, pos=pos, pre=pre, lens=lens)
+
+
+def _pairs(p):
+    n = p["lens"].astype(np.int64)
+    return int((n * (n + 1) // 2 + np.where(p["pre"] < 0, 0, n * n[p["pre"]])).sum())
+
+
+def _spans(case):
+    """Tokens [cu[s], cu[s+1]) of each sequence of a policy case (odd lengths,
+    what is left after the last is padding), and how many of each sequence's
+    first tokens are its prompt."""
+    T, n = case["T"], case["seqs"]
+    cu = np.floor(np.linspace(0, T - T // 40, n + 1)).astype(np.int32)
+    prompt = np.floor((1.0 - case["answer"]) * np.diff(cu)).astype(np.int32)
+    return cu, prompt
+
+
+def work(case):
+    D = case.get("D", 0)
+    if case["kind"] == "front":
+        T, hs, hkv = case["T"], case["hs"], case["hkv"]
+        qm, km = _head_maps(case)
+        slots, heads = len(qm) + 2 * len(km), hs + 2 * hkv
+        if case["dir"] == "fwd":
+            return dict(bytes=2 * T * D * (heads + slots) + 4 * T, flops=12 * T * D * (hs + hkv))
+        read = (int((qm >= 0).sum()) + 2 * int((km >= 0).sum())) + (hs + hkv if case["norm"] else 0)
+        return dict(bytes=2 * T * D * (read + heads) + 4 * T, flops=24 * T * D * (hs + hkv))
+    if case["kind"] == "prefix":
+        p = _attn(case)
+        rows, keys = 2 * p["T"] * p["H"] * D, 2 * p["T"] * p["Hkv"] * D
+        lse = 4 * p["T"] * p["H"]
+        if case["dir"] == "fwd":
+            return dict(bytes=2 * rows + 2 * keys + lse, flops=4 * D * _pairs(p) * p["real"])
+        return dict(bytes=4 * rows + 4 * keys + lse, flops=10 * D * _pairs(p) * p["real"])
+    cu, prompt = _spans(case)
+    T, V, counted = case["T"], case["V"], int((np.diff(cu) - prompt).sum())
+    if case["dir"] == "fwd":
+        return dict(bytes=2 * counted * V + 24 * T, flops=5 * counted * V)
+    return dict(bytes=2 * (counted + T) * V + 24 * T, flops=6 * counted * V)
+
+
+# ------------------------------------------------------------------- inputs
+def _randn(gen, *shape, scale=1.0):
+    return (torch.randn(shape, generator=gen, device=DEV, dtype=torch.float32) * scale).to(torch.bfloat16)
+
+
+def _dev(a, dtype):
+    return torch.as_tensor(np.asarray(a), dtype=dtype).to(DEV)
+
+
+def _inputs(case, seed):
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(int(seed))
+    if case["kind"] == "front":
+        T, D, hs, hkv, n = case["T"], case["D"], case["hs"], case["hkv"], case["sp"]
+        # one projection holds a token's query, key and value heads
+        qkv = _randn(gen, T, hs + 2 * hkv, D)
+        x = dict(q=qkv[:, :hs], k=qkv[:, hs:hs + hkv], v=qkv[:, hs + hkv:],
+                 pos=torch.arange(case["base"], case["base"] + T, device=DEV, dtype=torch.int32), wq=None, wk=None)
+        if case["norm"]:
+            x.update(wq=(1 + 0.2 * _randn(gen, D)), wk=(1 + 0.2 * _randn(gen, D)))
+        if case["dir"] == "bwd":
+            qm, km = _head_maps(case)
+            x.update({a: _randn(gen, n, T, len(m) // n, D) for a, m in (("dq", qm), ("dk", km), ("dv", km))})
+        return x
+    if case["kind"] == "prefix":
+        p = _attn(case)
+        T, D = p["T"], p["D"]
+        x = dict(q=_randn(gen, T, p["H"], D), k=_randn(gen, T, p["Hkv"], D), v=_randn(gen, T, p["Hkv"], D))
+        x["q"][:, p["real"]:] = 0  # dummy slots arrive as zeros
+        if case["dir"] == "bwd":
+            x["do"] = _randn(gen, T, p["H"], D)
+            x["do"][:, p["real"]:] = 0
+        return x
+    T, V = case["T"], case["V"]
+    cu, prompt = _spans(case)
+    x = dict(logits=torch.empty((T, V), dtype=torch.bfloat16, device=DEV))
+    for t in range(0, T, 512):
+        x["logits"][t:t + 512] = _randn(gen, min(512, T - t), V, scale=2.0)
+    label = torch.randint(0, V, (T,), generator=gen, device=DEV)
+    # a sampled token is a likely one: its logit is near the row's log-sum
+    near = math.log(V) + 2.0 + torch.randn(T, generator=gen, device=DEV)
+    x["logits"].scatter_(1, label[:, None], near[:, None].to(torch.bfloat16))
+    counted = np.zeros(T, bool)
+    for a, b, m in zip(cu[:-1], cu[1:], prompt):
+        counted[a + m:b] = True
+    x["labels"] = torch.where(_dev(counted, torch.bool), label, torch.full_like(label, -100)).to(torch.int32)
+    logp = torch.empty(T, dtype=torch.float64, device=DEV)
+    lse, ent = torch.empty_like(logp), torch.empty_like(logp)
+    for t in range(0, T, 256):
+        z = x["logits"][t:t + 256].double()
+        top = z.max(1, keepdim=True).values
+        e = (z - top).exp()
+        s = e.sum(1, keepdim=True)
+        lse[t:t + 256] = (top + s.log())[:, 0]
+        ent[t:t + 256] = lse[t:t + 256] - (e * z).sum(1) / s[:, 0]
+        logp[t:t + 256] = z.gather(1, label[t:t + 256, None])[:, 0] - lse[t:t + 256]
+    # the sampling model's and the reference's log-probabilities of the same
+    # tokens; no ratio lies within 1e-3 of a border of the clip, where a rounding
+    # would decide
+    ratio = 0.15 * torch.randn(T, generator=gen, device=DEV, dtype=torch.float64)
+    for edge in (math.log(1 - CLIP[0]), math.log(1 + CLIP[1])):
+        ratio = torch.where((ratio - edge).abs() < 1e-3, ratio + 2.5e-3, ratio)
+    x["old"] = (logp - ratio).float()
+    x["ref"] = (logp + 0.3 * torch.randn(T, generator=gen, device=DEV, dtype=torch.float64)).float()
+    x["adv"] = torch.randn(T if case["per_token"] else case["seqs"], generator=gen, device=DEV)
+    live = x["labels"] >= 0
+    for name, v in (("logp", logp), ("lse", lse), ("ent", ent)):
+        x[name] = torch.where(live, v, torch.zeros_like(v)).float()
+    # the gradient of each sequence's sum, as a mean over the batch's tokens gives it
+    x["grad"] = 1.0 / (1 + torch.rand(case["seqs"], generator=gen, device=DEV) + T)
+    return x
+
+
+CLIP = (0.2, 0.28)  # ratios in [0.8, 1.28] count
+
+
+def _visible(p, rows=slice(None)):
+    """[rows, T] truth values: which keys a row sees."""
+    seg = np.repeat(np.arange(len(p["lens"])), p["lens"])
+    s, t, pos = _dev(seg, torch.int64), _dev(p["pre"][seg], torch.int64), _dev(p["pos"], torch.int64)
+    return ((s[rows, None] == s[None]) & (pos[None] <= pos[rows, None])) | (t[rows, None] == s[None])
+
+
+def prepare(case, seed):
+    x = _inputs(case, seed)
+    s = dict(case=dict(case), x=x)
+    if case["kind"] == "front":
+        qm, km = _head_maps(case)
+        s.update(qm=_dev(qm, torch.int64), km=_dev(km, torch.int64), freqs=_dev(_freqs(case), torch.float64))
+    elif case["kind"] == "prefix":
+        p = s["p"] = _attn(case)
+        s.update(kv=_dev(p["kv"], torch.int64))
+        if case["dir"] == "bwd":  # what the forward left
+            o = torch.zeros(p["T"], p["H"], p["D"], device=DEV)
+            lse = torch.full((p["H"], p["T"]), -math.inf, device=DEV)
+            for a in range(0, p["T"], 2048):
+                see = _visible(p, slice(a, a + 2048))
+                for h in range(p["real"]):
+                    z = x["q"][a:a + 2048, h].float() @ x["k"][:, p["kv"][h]].float().t().contiguous() / math.sqrt(p["D"])
+                    z.masked_fill_(~see, -math.inf)
+                    lse[h, a:a + 2048] = z.logsumexp(1)
+                    o[a:a + 2048, h] = (z - lse[h, a:a + 2048, None]).exp() @ x["v"][:, p["kv"][h]].float()
+            x.update(o=o.to(torch.bfloat16), lse=lse)
+    else:
+        s["cu"] = _spans(case)[0]
+    if own:  # the description a program makes once a batch and keeps for its layers
+        import paper_2505_22296_amd as sp
+        if case["kind"] == "front":
+            s["desc"] = sp.QkDesc(T=case["T"], head_dim=case["D"], H_q=case["hs"], H_kv=case["hkv"], sp=case["sp"],
+                                  q_map=qm, kv_map=km, rotary_dim=case["rot"], inv_freq=_freqs(case),
+                                  interleaved=case["pairs"] == "neighbours", eps=EPS)
+        elif case["kind"] == "prefix":
+            s["desc"] = sp.Desc(T_q=p["T"], T_k=p["T"], head_dim=p["D"], cu_seqlens_q=p["cu"], cu_seqlens_k=p["cu"],
+                                position_ids_q=p["pos"], position_ids_k=p["pos"], prefix_of=p["pre"], **p["heads"])
+    return s
+
+
+# ------------------------------------------------------------ one pass of a case
+def run(s):
+    c, x = s["case"], s["x"]
+    if own:
+        return _own(s)
+    if c["kind"] == "front":
+        return _front_fwd(s) if c["dir"] == "fwd" else _front_bwd(s)
+    if c["kind"] == "prefix":
+        return _prefix_fwd(s) if c["dir"] == "fwd" else _prefix_bwd(s)
+    return _policy_fwd(c, x, s["cu"]) if c["dir"] == "fwd" else _policy_bwd(c, x, s["cu"])
+
+
+def _own(s):
+    import paper_2505_22296_amd as sp
+    c, x = s["case"], s["x"]
+    if c["kind"] == "front":
+        if c["dir"] == "fwd":
+            q, k, v = sp.sp_qk_norm_rope(s["desc"], x["q"], x["k"], x["v"], x["pos"], x["wq"], x["wk"])
+            return dict(q=q, k=k, v=v)
+        dq, dk, dv, dwq, dwk = sp.sp_qk_norm_rope_bwd(s["desc"], x["q"], x["k"], x["dq"], x["dk"], x["dv"], x["pos"],
+                                                      x["wq"], x["wk"])
+        out = dict(dq=dq, dk=dk, dv=dv)
+        return dict(out, dwq=dwq, dwk=dwk) if c["norm"] else out
+    if c["kind"] == "prefix":
+        if c["dir"] == "fwd":
+            o, lse = sp.sp_attn_fwd(s["desc"], x["q"], x["k"], x["v"])
+            return dict(o=o, lse=lse)
+        dq, dk, dv = sp.sp_attn_bwd(s["desc"], x["q"], x["k"], x["v"], x["o"], x["lse"], x["do"])
+        return dict(dq=dq, dk=dk, dv=dv)
+    p = sp.PolicyParams(clip_low=CLIP[0], clip_high=CLIP[1], kl_coef=c["kl"], entropy_coef=c["ent"])
+    if c["dir"] == "fwd":
+        logp, lse, ent, sums, stats = sp.sp_policy_loss(p, x["logits"], x["labels"], x["old"], x["ref"], x["adv"], s["cu"])
+        return dict(logp=logp, lse=lse, ent=ent, sums=sums, stats=stats)
+    return dict(dlogits=sp.sp_policy_loss_bwd(p, x["logits"], x["labels"], x["logp"], x["lse"], x["ent"], x["old"], x["ref"],
+                                              x["adv"], s["cu"], x["grad"]))
+
+
+# ---------------------------------------------------------- front, plain form
+def _turn(y, cos, sin, c):
+    """Pairs of the first `rot` dims of y [T, H, D] turned by the angles."""
+    R = c["rot"]
+    if c["pairs"] == "halves":
+        a, b = y[..., :R // 2], y[..., R // 2:R]
+        r = torch.cat([a * cos - b * sin, a * sin + b * cos], -1)
+    else:
+        a, b = y[..., 0:R:2], y[..., 1:R:2]
+        r = torch.stack([a * cos - b * sin, a * sin + b * cos], -1).flatten(-2)
+    return torch.cat([r, y[..., R:]], -1)
+
+
+def _angles(s):
+    a = s["x"]["pos"].double()[:, None] * s["freqs"]
+    return a.cos().float()[:, None], a.sin().float()[:, None]
+
+
+def _norm(x, w):
+    return x * torch.rsqrt((x * x).mean(-1, keepdim=True) + EPS) * w.float()
+
+
+def _to_slots(y, m, n):
+    """[T, H, D] -> [n, T, slots a rank, D], zeros where the map has -1."""
+    y = torch.cat([y, torch.zeros_like(y[:, :1])], 1)[:, m]
+    return y.reshape(y.shape[0], n, -1, y.shape[2]).transpose(0, 1).contiguous()
+
+
+def _from_slots(g, m, H):
+    """[n, T, slots a rank, D] -> [T, H, D] float32, copies of a head summed."""
+    g = g.transpose(0, 1).flatten(1, 2).float()
+    return torch.zeros(g.shape[0], H + 1, g.shape[2], device=g.device).index_add_(1, m % (H + 1), g)[:, :H]
+
+
+def _front_fwd(s):
+    c, x = s["case"], s["x"]
+    cos, sin = _angles(s)
+    q, k = x["q"].float(), x["k"].float()
+    if c["norm"]:
+        q, k = _norm(q, x["wq"]), _norm(k, x["wk"])
+    bf = torch.bfloat16
+    return dict(q=_to_slots(_turn(q, cos, sin, c).to(bf), s["qm"], c["sp"]),
+                k=_to_slots(_turn(k, cos, sin, c).to(bf), s["km"], c["sp"]), v=_to_slots(x["v"], s["km"], c["sp"]))
+
+
+def _norm_bwd(x, w, dy):
+    r = torch.rsqrt((x * x).mean(-1, keepdim=True) + EPS)
+    n = x * r
+    g = dy * w.float()
+    return r * (g - n * (g * n).mean(-1, keepdim=True)), (dy * n).sum((0, 1))
+
+
+def _front_bwd(s):
+    c, x = s["case"], s["x"]
+    cos, sin = _angles(s)
+    dq = _turn(_from_slots(x["dq"], s["qm"], c["hs"]), cos, -sin, c)
+    dk = _turn(_from_slots(x["dk"], s["km"], c["hkv"]), cos, -sin, c)
+    out = dict(dv=_from_slots(x["dv"], s["km"], c["hkv"]).to(torch.bfloat16))
+    if c["norm"]:
+        dq, out["dwq"] = _norm_bwd(x["q"].float(), x["wq"], dq)
+        dk, out["dwk"] = _norm_bwd(x["k"].float(), x["wk"], dk)
+    return dict(out, dq=dq.to(torch.bfloat16), dk=dk.to(torch.bfloat16))
+
+
+# --------------------------------------------------------- prefix, plain form
+def _heads(t, index):
+    """[T, H, D] -> [heads of the index, T, D] float32."""
+    return t.float()[:, index].transpose(0, 1).contiguous()
+
+
+def _scores(s):
+    p, x = s["p"], s["x"]
+    q = _heads(x["q"], slice(p["real"]))
+    k = _heads(x["k"], s["kv"])
+    z = torch.matmul(q, k.transpose(1, 2).contiguous()).mul_(1.0 / math.sqrt(p["D"]))
+    return q, k, z.masked_fill_(~_visible(p), -math.inf)
+
+
+def _prefix_fwd(s):
+    p, x = s["p"], s["x"]
+    _, _, z = _scores(s)
+    top = z.max(-1, keepdim=True).values  # (every row sees itself)
+    e = z.sub_(top).exp_()
+    total = e.sum(-1, keepdim=True)
+    o = torch.zeros(p["T"], p["H"], p["D"], device=DEV)
+    o[:, :p["real"]] = (torch.matmul(e, _heads(x["v"], s["kv"])) / total).transpose(0, 1)
+    lse = torch.full((p["H"], p["T"]), -math.inf, device=DEV)
+    lse[:p["real"]] = (top + total.log())[..., 0]
+    return dict(o=o.to(torch.bfloat16), lse=lse)
+
+
+def _prefix_bwd(s):
+    p, x = s["p"], s["x"]
+    q, k, z = _scores(s)
+    n = slice(p["real"])
+    v, do, o = _heads(x["v"], s["kv"]), _heads(x["do"], n), _heads(x["o"], n)
+    e = z.sub_(x["lse"][n, :, None]).exp_()
+    dv = torch.matmul(e.transpose(1, 2).contiguous(), do)
+    dz = torch.matmul(do, v.transpose(1, 2).contiguous()).sub_((do * o).sum(-1, keepdim=True)).mul_(e)
+    del e, z
+    scale = 1.0 / math.sqrt(p["D"])
+    dq = torch.zeros(p["T"], p["H"], p["D"], device=DEV)
+    dq[:, n] = torch.matmul(dz, k).mul_(scale).transpose(0, 1)
+    dk = torch.matmul(dz.transpose(1, 2).contiguous(), q).mul_(scale)
+
+    def of_kv(g):  # summed over the query heads that read a KV head
+        at = torch.zeros(p["Hkv"], p["T"], p["D"], device=DEV).index_add_(0, s["kv"], g)
+        return at.transpose(0, 1).to(torch.bfloat16).contiguous()
+    return dict(dq=dq.to(torch.bfloat16), dk=of_kv(dk), dv=of_kv(dv))
+
+
+# --------------------------------------------------------- policy, plain form
+def _of_tokens(c, x, cu):
+    """Each token's sequence (`seqs`: none), advantage, and whether it counts."""
+    t = torch.arange(c["T"], device=DEV)
+    seq = torch.bucketize(t, _dev(cu[1:], torch.int64), right=True)
+    live = (seq < c["seqs"]) & (x["labels"] >= 0)
+    seq = torch.where(live, seq, torch.full_like(seq, c["seqs"]))
+    return seq, x["adv"] if c["per_token"] else torch.cat([x["adv"], x["adv"][:1]])[seq], live
+
+
+def _policy_fwd(c, x, cu):
+    seq, adv, live = _of_tokens(c, x, cu)
+    z = x["logits"].float()
+    top = z.max(1, keepdim=True).values
+    z = z - top
+    e = z.exp()
+    total = e.sum(1, dtype=torch.float64)
+    lsum = total.log()
+    of_label = z.gather(1, x["labels"].clamp(min=0).long()[:, None])[:, 0].double()
+    logp = of_label - lsum
+    ent = lsum - (e * z).sum(1, dtype=torch.float64) / total
+    lse = top[:, 0].double() + lsum
+    # (the terms in 64 bits: e^d - d - 1 of a small d)
+    ratio = (logp - x["old"]).exp()
+    held = ratio.clamp(1 - CLIP[0], 1 + CLIP[1])
+    pg = -torch.minimum(ratio * adv, held * adv)
+    d = x["ref"] - logp
+    kl = d.exp() - d - 1
+    clipped = (ratio * adv > held * adv).double()
+    term = pg + c["kl"] * kl - c["ent"] * ent
+    zero = torch.zeros_like(term)
+
+    def sums(v):
+        return torch.zeros(c["seqs"] + 1, device=DEV, dtype=torch.float64).index_add_(0, seq, torch.where(live, v, zero))[:-1]
+    return dict(logp=torch.where(live, logp, zero).float(), lse=torch.where(live, lse, zero).float(),
+                ent=torch.where(live, ent, zero).float(), sums=sums(term).float(),
+                stats=torch.stack([sums(kl), sums(ent), sums(clipped), sums(zero + 1)], 1).float())
+
+
+def _policy_bwd(c, x, cu):
+    seq, adv, live = _of_tokens(c, x, cu)
+    ratio = (x["logp"] - x["old"]).exp()
+    inside = torch.where(adv >= 0, ratio <= 1 + CLIP[1], ratio >= 1 - CLIP[0])
+    up = torch.where(live, torch.cat([x["grad"], x["grad"][:1]])[seq], torch.zeros_like(ratio))
+    g = up * (torch.where(inside, -adv * ratio, torch.zeros_like(ratio)) - c["kl"] * torch.expm1(x["ref"] - x["logp"]))
+    lp = x["logits"].float().sub_(x["lse"][:, None])
+    if c["ent"]:
+        coef = (lp + x["ent"][:, None]).mul_((up * c["ent"])[:, None]).sub_(g[:, None])
+        d = lp.exp_().mul_(coef)
+    else:
+        d = lp.exp_().mul_(-g[:, None])
+    d.scatter_add_(1, x["labels"].clamp(min=0).long()[:, None], g[:, None])
+    return dict(dlogits=d.masked_fill_(~live[:, None], 0.0).to(torch.bfloat16))
+
+
+# -------------------------------------------------------- results in 64 bits
+def exact(case, seed):
+    s = prepare(case, seed)
+    if case["kind"] == "front":
+        return _exact_front(case, s["x"])
+    if case["kind"] == "prefix":
+        return _exact_prefix(s)
+    return _exact_policy(case, s)
+
+
+def _exact_front(c, x):
+    """Pairs as complex numbers, multiplied by exp(i angle); the norm's backward
+    through its matrix."""
+    R, D = c["rot"], c["D"]
+    f = np.float64(THETA) ** (-np.arange(0, R, 2, dtype=np.float64) / R)
+    angle = torch.outer(x["pos"].double(), torch.from_numpy(f).to(DEV))
+    unit = torch.polar(torch.ones_like(angle), angle)[:, None]
+    qm, km = _head_maps(c)
+    halves = c["pairs"] == "halves"
+
+    def turned(y, u):
+        z = y[..., :R].unflatten(-1, (2, R // 2)).movedim(-2, -1) if halves else y[..., :R].unflatten(-1, (R // 2, 2))
+        z = torch.view_as_real(torch.view_as_complex(z.contiguous()) * u)
+        return torch.cat([(z.movedim(-1, -2) if halves else z).flatten(-2), y[..., R:]], -1)
+
+    def packed(y, m):
+        n = c["sp"]
+        out = torch.zeros(n, c["T"], len(m) // n, D, dtype=torch.float64, device=DEV)
+        for i, h in enumerate(m):
+            if h >= 0:
+                out[i // (len(m) // n), :, i % (len(m) // n)] = y[:, h]
+        return out
+
+    def unpacked(g, m, H):
+        n = c["sp"]
+        out = torch.zeros(c["T"], H, D, dtype=torch.float64, device=DEV)
+        for i, h in enumerate(m):
+            if h >= 0:
+                out[:, h] += g[i // (len(m) // n), :, i % (len(m) // n)].double()
+        return out
+
+    def rms(y):
+        return (torch.linalg.vector_norm(y, dim=-1, keepdim=True) ** 2 / D + EPS).sqrt()
+    q, k = x["q"].double(), x["k"].double()
+    if c["dir"] == "fwd":
+        if c["norm"]:
+            q, k = q / rms(q) * x["wq"].double(), k / rms(k) * x["wk"].double()
+        return dict(q=packed(turned(q, unit), qm), k=packed(turned(k, unit), km), v=packed(x["v"].double(), km))
+    out = dict(dv=unpacked(x["dv"], km, c["hkv"]))
+    for name, y, w, m, H in (("q", q, x["wq"], qm, c["hs"]), ("k", k, x["wk"], km, c["hkv"])):
+        dy = turned(unpacked(x["d" + name], m, H), unit.conj())
+        if c["norm"]:
+            r = rms(y)
+            out["dw" + name] = (dy * y / r).sum(0).sum(0)
+            g = dy * w.double()
+            dy = g / r - y * ((g * y).sum(-1, keepdim=True) / (D * r ** 3))
+        out["d" + name] = dy
+    return out
+
+
+def _exact_prefix(s):
+    """Segment by segment: the keys of the prompt and of the answer side by side."""
+    p, x, c = s["p"], s["x"], s["case"]
+    T, D, scale = p["T"], p["D"], 1.0 / math.sqrt(p["D"])
+
+    def zeros(H):
+        return torch.zeros(T, H, D, dtype=torch.float64, device=DEV)
+    o, dq, dk, dv = zeros(p["H"]), zeros(p["H"]), zeros(p["Hkv"]), zeros(p["Hkv"])
+    lse = torch.full((p["H"], T), -math.inf, dtype=torch.float64, device=DEV)
+    for h in range(p["real"]):
+        q, k, v = x["q"][:, h].double(), x["k"][:, p["kv"][h]].double(), x["v"][:, p["kv"][h]].double()
+        for i, pre in enumerate(p["pre"]):
+            b, e = int(p["cu"][i]), int(p["cu"][i + 1])
+            for r in range(b, e, 4096):
+                at = torch.arange(r, min(r + 4096, e), device=DEV)
+                keys = torch.arange(b, int(at[-1]) + 1, device=DEV)
+                if pre >= 0:
+                    keys = torch.cat([torch.arange(int(p["cu"][pre]), int(p["cu"][pre + 1]), device=DEV), keys])
+                z = q[at] @ k[keys].T * scale
+                z = torch.where((keys[None] >= b) & (keys[None] > at[:, None]), -math.inf, z)
+                if c["dir"] == "fwd":
+                    lse[h, at] = torch.logsumexp(z, 1)
+                    o[at, h] = torch.softmax(z, 1) @ v[keys]
+                    continue
+                w = torch.exp(z - x["lse"][h, at].double()[:, None])
+                do = x["do"][at, h].double()
+                dz = w * (do @ v[keys].T - (do * x["o"][at, h].double()).sum(1, keepdim=True)) * scale
+                dq[at, h] = dz @ k[keys]
+                dk[keys, p["kv"][h]] += dz.T @ q[at]
+                dv[keys, p["kv"][h]] += w.T @ do
+    return dict(o=o, lse=lse) if c["dir"] == "fwd" else dict(dq=dq, dk=dk, dv=dv)
+
+
+def _exact_policy(c, s):
+    """Token by token from log_softmax; the gradient through autograd of the
+    summed terms, a block of rows at a time."""
+    x, cu = s["x"], s["cu"]
+    names = ("logp", "lse", "ent", "clip", "kl", "term")
+    v = {n: np.zeros(c["T"]) for n in names}
+    dl = torch.zeros(c["T"], c["V"], dtype=torch.float64, device=DEV) if c["dir"] == "bwd" else None
+    labels = x["labels"].cpu().numpy()
+    seq = np.searchsorted(cu, np.arange(c["T"]), side="right") - 1
+    rows = np.flatnonzero((labels >= 0) & (seq < c["seqs"]))
+    adv = x["adv"].double()
+    for a in range(0, len(rows), 512):
+        r = rows[a:a + 512]
+        at, of = torch.from_numpy(r).to(DEV), torch.from_numpy(seq[r]).to(DEV)
+        z = x["logits"][at].double()
+        A = adv[at] if c["per_token"] else adv[of]
+        lab = x["labels"][at].long()[:, None]
+        if c["dir"] == "bwd":
+            # the operator's inputs: its own log-probabilities decide ratio and KL
+            lp = x["logp"][at].double().requires_grad_()
+            ratio = torch.exp(lp - x["old"][at].double())
+            term = -torch.minimum(ratio * A, ratio.clamp(1 - CLIP[0], 1 + CLIP[1]) * A)
+            d = x["ref"][at].double() - lp
+            term = term + c["kl"] * (torch.expm1(d) - d)
+            G = x["grad"].double()[of]
+            g, = torch.autograd.grad((G * term).sum(), lp)
+            logq = z - x["lse"][at].double()[:, None]
+            prob = torch.exp(logq)
+            d = -g[:, None] * prob
+            if c["ent"]:
+                d += (G * c["ent"])[:, None] * prob * (logq + x["ent"][at].double()[:, None])
+            dl[at] = d.scatter_add(1, lab, g[:, None])
+            continue
+        logq = torch.log_softmax(z, 1)
+        lp = logq.gather(1, lab)[:, 0]
+        ent = -(torch.exp(logq) * logq).sum(1)
+        ratio = torch.exp(lp - x["old"][at].double())
+        held = ratio.clamp(1 - CLIP[0], 1 + CLIP[1])
+        d = x["ref"][at].double() - lp
+        kl = torch.expm1(d) - d
+        term = torch.maximum(-ratio * A, -held * A) + c["kl"] * kl - c["ent"] * ent
+        for n, y in zip(names, (lp, torch.logsumexp(z, 1), ent, (ratio * A > held * A).double(), kl, term)):
+            v[n][r] = y.cpu().numpy()
+    if c["dir"] == "bwd":
+        return dict(dlogits=dl)
+
+    def sums(y):
+        return np.bincount(seq[rows], y[rows], minlength=c["seqs"])
+    return dict(logp=v["logp"], lse=v["lse"], ent=v["ent"], sums=sums(v["term"]),
+                stats=np.stack([sums(v["kl"]), sums(v["ent"]), sums(v["clip"]), sums(np.ones(c["T"]))], 1))
