@@ -339,7 +339,8 @@ def _own(s):
             return dict(o=o, lse=lse)
         dq, dk, dv = sp.sp_attn_bwd(s["desc"], x["q"], x["k"], x["v"], x["o"], x["lse"], x["do"])
         return dict(dq=dq, dk=dk, dv=dv)
-    p = sp.PolicyParams(clip_low=CLIP[0], clip_high=CLIP[1], kl_coef=c["kl"], entropy_coef=c["ent"])
+    p = sp.PolicyParams(clip_low=CLIP[0], clip_high=CLIP[1], kl_coef=c["kl"], entropy_coef=c["ent"],
+                        adv_per_token=c["per_token"])
     if c["dir"] == "fwd":
         logp, lse, ent, sums, stats = sp.sp_policy_loss(p, x["logits"], x["labels"], x["old"], x["ref"], x["adv"], s["cu"])
         return dict(logp=logp, lse=lse, ent=ent, sums=sums, stats=stats)
