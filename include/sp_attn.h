@@ -463,6 +463,136 @@ sp_status sp_loss_reduce(const float* partial_sums, const float* ref_partial_sum
                          void* stream);
 
 /*
+ * Clipped policy loss with a KL and an entropy term over one rank's tokens, from
+ * the logits (next to sp_token_logprob, for training on sampled answers).  A token
+ * t counts if its label y = labels[t] is in [0, V) and not ignore_index and a
+ * sequence s holds t.  With A = advantages[adv_per_token ? t : s]:
+ *   lse[t]     = log sum_v exp(logits[t, v])          (float32, natural log)
+ *   logp[t]    = logits[t, y] - lse[t]
+ *   entropy[t] = -sum_v p_v log p_v
+ *   r = exp(logp - old_logp[t]),  pg = -min(r A, min(max(r, 1 - clip_low), 1 + clip_high) A)
+ *   d = ref_logp[t] - logp,       kl = exp(d) - d - 1
+ *   seq_sum[s] = sum over s's counted tokens of pg + kl_coef kl - entropy_coef entropy
+ *   seq_stats[s] = {sum of kl, sum of entropy, tokens whose ratio the clip holds
+ *                   (r A > the clipped one), counted tokens}
+ * Other tokens get 0 in logp, lse and entropy, and their logits are not read.  The
+ * sums are what sp_loss_reduce takes as a rank's partial sums (SP_LOSS_SFT with
+ * coef = -1 / n gives their mean over n); sequences without counted tokens get 0.
+ * A token's values are formed in float64 from float32 sums over its row and the
+ * sums over tokens in float64 in a fixed order: repeating a call gives the same
+ * bits.  A logit of -inf has probability 0; a row of nothing above -6.9e29 has lse
+ * = logp = -inf and entropy 0; +inf or NaN in a counted row make the token's values
+ * NaN.  r A counts as 0 where A is 0.
+ *
+ * logits: DEVICE bf16 [T, V] row-major, 16-byte aligned, V a multiple of 8; labels:
+ * DEVICE int32 [T]; old_logp, ref_logp: DEVICE float32 [T], ref_logp may be NULL
+ * (kl = 0; kl_coef must be 0); advantages: DEVICE float32 [T] or [num_seqs];
+ * cu_seqlens: HOST as in sp_token_logprob; logp, lse, entropy: DEVICE float32 [T],
+ * entropy may be NULL (entropy_coef must be 0); seq_sum [num_seqs] and seq_stats
+ * [num_seqs, SP_POLICY_STATS] DEVICE float32.  clip_low in [0, 1], clip_high >= 0,
+ * coefficients finite (SP_ERR_INVALID_ARG).  Workspace: sp_policy_workspace_size.
+ * Limits: num_seqs <= 256, T < 2^24 (SP_ERR_UNSUPPORTED).  Reads the counted rows
+ * once.
+ */
+typedef struct sp_policy_params {
+  float clip_low, clip_high;     /* the ratio counts inside [1 - clip_low, 1 + clip_high] */
+  float kl_coef, entropy_coef;
+  int32_t adv_per_token;         /* advantages: 1 = [T], 0 = [num_seqs]                   */
+  int32_t ignore_index;
+} sp_policy_params;
+#define SP_POLICY_STATS 4
+sp_status sp_policy_workspace_size(int32_t T, int32_t V, size_t* bytes);
+sp_status sp_policy_loss(const sp_policy_params* params, const void* logits, const int32_t* labels,
+                         const float* old_logp, const float* ref_logp, const float* advantages,
+                         int32_t T, int32_t V, const int32_t* cu_seqlens, int32_t num_seqs,
+                         float* logp, float* lse, float* entropy, float* seq_sum,
+                         float* seq_stats, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Backward of sum_s grad_seq[s] * seq_sum[s] to the logits (DEVICE bf16 [T, V]
+ * out; it may be the logits buffer itself): for a counted token of sequence s, with
+ * G = grad_seq[s] and p_v = exp(logits[t, v] - lse[t]),
+ *   g = G (dpg + kl_coef (1 - exp(ref_logp[t] - logp[t]))),
+ *   dpg = -A r where the clip does not hold r (r <= 1 + clip_high for A >= 0,
+ *         r >= 1 - clip_low for A < 0), else 0
+ *   dlogits[t, v] = g (1[v == y] - p_v) + G entropy_coef p_v (log p_v + entropy[t])
+ * rounded to bf16 (nearest-even); every other row, and a row with lse = -inf, is
+ * written as zeros and not read.  logp, lse, entropy: what sp_policy_loss wrote
+ * (entropy may be NULL if entropy_coef is 0); grad_seq: DEVICE float32 [num_seqs].
+ * Same shape rules as sp_policy_loss; needs no workspace.
+ */
+sp_status sp_policy_loss_bwd(const sp_policy_params* params, const void* logits,
+                             const int32_t* labels, const float* logp, const float* lse,
+                             const float* entropy, const float* old_logp, const float* ref_logp,
+                             const float* advantages, int32_t T, int32_t V,
+                             const int32_t* cu_seqlens, int32_t num_seqs, const float* grad_seq,
+                             void* dlogits, void* stream);
+
+/*
+ * Norms of the query and key heads, rotation by position, and the pack for the
+ * all-to-all (sp_ulysses_pack's layout) in one pass, for Q, K and V of one rank's
+ * token slice.  For token t and slot h of rank j with head g = map[j*H_loc + h]:
+ *   n = x[t, g, :] / sqrt(mean(x[t, g, :]^2) + eps) * (w + weight_offset)
+ *       (n = x where w_q, for the keys w_k, is NULL)
+ *   the pairs (n_i, n_{i + rotary_dim/2}) -- interleaved: (n_2i, n_2i+1) -- of the
+ *   first rotary_dim dims are turned by position * inv_freq[i] radians and scaled
+ *   by rope_scale; the other dims stay
+ *   dst[j, t, h, :] = bf16 of that, +0 where the map has -1.
+ * V's heads take K's map and are copied bit by bit.  Computed in float32, rounded
+ * once; angles are exact to 2^-32 turns and a float32 rounding at any position.
+ *
+ * q: DEVICE bf16, token t at q + t * q_stride (in elements), its H_q heads of
+ * head_dim next to each other; k, v the same with H_kv heads: three tensors, or
+ * parts of one projection's output.  Strides are multiples of 8 and hold the
+ * heads; every tensor is 16-byte aligned.  positions: DEVICE int32 [T], or NULL:
+ * token t is at position_base + t.  w_q, w_k: DEVICE bf16 [head_dim] or NULL.
+ * q_dst: [sp, T, Hq_loc, D]; k_dst, v_dst: [sp, T, Hkv_loc, D] bf16, contiguous,
+ * written.  inv_freq and the maps: HOST, read during the call; any finite
+ * frequency.  head_dim 64 or 128; rotary_dim a multiple of 16 up to head_dim, 0 for
+ * no rotation; maps as in sp_ulysses_pack.  Limits: sp*Hq_loc, sp*Hkv_loc <= 512,
+ * H_q, H_kv <= 256, T < 2^24 (SP_ERR_UNSUPPORTED).  T == 0 is a no-op.  May be
+ * captured into a graph.
+ */
+typedef struct sp_qk_desc {
+  int32_t T, head_dim, H_q, H_kv;
+  int32_t sp, Hq_loc, Hkv_loc;
+  int32_t rotary_dim, interleaved, position_base;
+  float rope_scale, eps, weight_offset;
+  const int32_t* q_map;    /* HOST, sp * Hq_loc entries in [-1, H_q)   */
+  const int32_t* kv_map;   /* HOST, sp * Hkv_loc entries in [-1, H_kv) */
+  const double* inv_freq;  /* HOST, rotary_dim / 2                     */
+} sp_qk_desc;
+sp_status sp_qk_norm_rope(const sp_qk_desc* desc, const void* q, int64_t q_stride, const void* k,
+                          int64_t k_stride, const void* v, int64_t v_stride,
+                          const int32_t* positions, const void* w_q, const void* w_k, void* q_dst,
+                          void* k_dst, void* v_dst, void* stream);
+
+/*
+ * Its backward, from the gradients as the reverse all-to-all leaves them:
+ * dq_src [sp, T, Hq_loc, D], dk_src, dv_src [sp, T, Hkv_loc, D] bf16 (chunk j came
+ * from rank j).  A head's gradients are summed over its slots in ascending order in
+ * float32 (as sp_ulysses_unpack_add does, without the rounding in between), turned
+ * back, and taken through the norm:
+ *   dq, dk, dv: DEVICE bf16, written, token t at dq + t * dq_stride and so on (the
+ *     strides' rules are those of q, k, v; a head in no slot gets +0); dq and dk may
+ *     be the q and k buffers themselves, with their strides
+ *   dw_q, dw_k: DEVICE float32 [head_dim], the gradients of w_q and w_k, written;
+ *     required where w_q (w_k) is given and NULL where it is not.
+ * q and k are read where their weight is given and may be NULL where it is not.
+ * Workspace (sp_qk_workspace_size): partial weight gradients, summed in a fixed
+ * order, so that repeating a call gives the same bits; not touched where neither
+ * weight is given.  T == 0 writes dw = 0.
+ */
+sp_status sp_qk_workspace_size(const sp_qk_desc* desc, size_t* bytes);
+sp_status sp_qk_norm_rope_bwd(const sp_qk_desc* desc, const void* q, int64_t q_stride,
+                              const void* k, int64_t k_stride, const void* dq_src,
+                              const void* dk_src, const void* dv_src, const int32_t* positions,
+                              const void* w_q, const void* w_k, void* dq, int64_t dq_stride,
+                              void* dk, int64_t dk_stride, void* dv, int64_t dv_stride,
+                              float* dw_q, float* dw_k, void* workspace, size_t workspace_bytes,
+                              void* stream);
+
+/*
  * Opt-in kernel timer (measurement support, per calling thread).  After
  * sp_profile_events(id, start, stop) with hipEvent_t handles created by the
  * caller, every launch of kernel `id` made by THIS thread records `start` on
@@ -481,7 +611,11 @@ enum {
   SP_KERNEL_LSE_MERGE = 6,/* standalone LSE merge                        */
   SP_KERNEL_UNPACK_ADD = 7,/* summing unpack of GQA K/V gradients        */
   SP_KERNEL_TOKEN_LOGPROB = 8,     /* token log-probabilities (forward)  */
-  SP_KERNEL_TOKEN_LOGPROB_BWD = 9  /* their backward to the logits       */
+  SP_KERNEL_TOKEN_LOGPROB_BWD = 9, /* their backward to the logits       */
+  SP_KERNEL_POLICY = 10,      /* policy loss: the pass over the logits   */
+  SP_KERNEL_POLICY_BWD = 11,  /* its backward to the logits              */
+  SP_KERNEL_QK_ROPE = 12,     /* norm, rotation and pack                 */
+  SP_KERNEL_QK_ROPE_BWD = 13  /* their backward                          */
 };
 sp_status sp_profile_events(int32_t kernel_id, void* start_event, void* stop_event);
 

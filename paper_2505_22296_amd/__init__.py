@@ -8,7 +8,10 @@ from ._lib import (Desc, SpError, load, status_string, sp_attn_workspace_size, s
                    sp_attn_fwd_static, STATIC_SCRATCH_BYTES,
                    sp_attn_bwd, sp_ring_step, sp_lse_merge, sp_f32_to_bf16, sp_profile_events,
                    sp_token_logprob, sp_token_logprob_bwd, sp_loss_reduce, SP_LOSS_SFT, SP_LOSS_DPO,
+                   PolicyParams, sp_policy_workspace_size, sp_policy_loss, sp_policy_loss_bwd,
+                   QkDesc, sp_qk_workspace_size, sp_qk_norm_rope, sp_qk_norm_rope_bwd,
                    SP_KERNEL_TOKEN_LOGPROB, SP_KERNEL_TOKEN_LOGPROB_BWD,
+                   SP_KERNEL_POLICY, SP_KERNEL_POLICY_BWD, SP_KERNEL_QK_ROPE, SP_KERNEL_QK_ROPE_BWD,
                    SP_OK, SP_ERR_INVALID_ARG, SP_ERR_UNSUPPORTED, SP_ERR_WORKSPACE, SP_ERR_HIP,
                    SP_OP_FWD, SP_OP_BWD, SP_OP_RING_STEP, SP_DESC_SINGLE_SEQUENCE, SP_DESC_ROWSTATS_READY,
                    SP_DESC_DQ_ACC_INIT,
@@ -22,7 +25,10 @@ __all__ = [
     "sp_attn_fwd_static", "STATIC_SCRATCH_BYTES",
     "sp_attn_bwd", "sp_ring_step", "sp_lse_merge", "sp_f32_to_bf16", "sp_profile_events",
     "sp_token_logprob", "sp_token_logprob_bwd", "sp_loss_reduce", "SP_LOSS_SFT", "SP_LOSS_DPO",
+    "PolicyParams", "sp_policy_workspace_size", "sp_policy_loss", "sp_policy_loss_bwd",
+    "QkDesc", "sp_qk_workspace_size", "sp_qk_norm_rope", "sp_qk_norm_rope_bwd",
     "SP_KERNEL_TOKEN_LOGPROB", "SP_KERNEL_TOKEN_LOGPROB_BWD",
+    "SP_KERNEL_POLICY", "SP_KERNEL_POLICY_BWD", "SP_KERNEL_QK_ROPE", "SP_KERNEL_QK_ROPE_BWD",
     "SP_OK", "SP_ERR_INVALID_ARG", "SP_ERR_UNSUPPORTED", "SP_ERR_WORKSPACE", "SP_ERR_HIP",
     "SP_OP_FWD", "SP_OP_BWD", "SP_OP_RING_STEP", "SP_DESC_SINGLE_SEQUENCE",
     "SP_DESC_ROWSTATS_READY", "SP_DESC_DQ_ACC_INIT", "EXPORTED",

@@ -43,6 +43,22 @@ class SpAttnDesc(ctypes.Structure):
     ]
 
 
+class SpPolicyParams(ctypes.Structure):
+    _fields_ = [("clip_low", ctypes.c_float), ("clip_high", ctypes.c_float), ("kl_coef", ctypes.c_float),
+                ("entropy_coef", ctypes.c_float), ("adv_per_token", ctypes.c_int32),
+                ("ignore_index", ctypes.c_int32)]
+
+
+class SpQkDesc(ctypes.Structure):
+    _fields_ = [
+        ("T", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("H_q", ctypes.c_int32), ("H_kv", ctypes.c_int32),
+        ("sp", ctypes.c_int32), ("Hq_loc", ctypes.c_int32), ("Hkv_loc", ctypes.c_int32),
+        ("rotary_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("position_base", ctypes.c_int32),
+        ("rope_scale", ctypes.c_float), ("eps", ctypes.c_float), ("weight_offset", ctypes.c_float),
+        ("q_map", _i32p), ("kv_map", _i32p), ("inv_freq", ctypes.POINTER(ctypes.c_double)),
+    ]
+
+
 class SpError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -63,7 +79,8 @@ def load() -> ctypes.CDLL:
         raise RuntimeError(f"{LIB_PATH} not built; run `python -m paper_2505_22296_amd.build`")
     lib = ctypes.CDLL(LIB_PATH)
     vp, i32, sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_size_t
-    D = ctypes.POINTER(SpAttnDesc)
+    i64 = ctypes.c_int64
+    D, P, Q = ctypes.POINTER(SpAttnDesc), ctypes.POINTER(SpPolicyParams), ctypes.POINTER(SpQkDesc)
     sig = {
         "sp_status_string": (ctypes.c_char_p, [i32]),
         "sp_version": (i32, []),
@@ -74,6 +91,13 @@ def load() -> ctypes.CDLL:
         "sp_token_logprob": (i32, [vp, vp, i32, i32, i32, vp, i32, vp, vp, vp, vp]),
         "sp_token_logprob_bwd": (i32, [vp, vp, vp, i32, i32, i32, vp, i32, vp, vp, vp]),
         "sp_loss_reduce": (i32, [vp, vp, i32, i32, i32, ctypes.c_float, vp, vp, vp]),
+        "sp_policy_workspace_size": (i32, [i32, i32, ctypes.POINTER(sz)]),
+        "sp_policy_loss": (i32, [P, vp, vp, vp, vp, vp, i32, i32, vp, i32, vp, vp, vp, vp, vp, vp, sz, vp]),
+        "sp_policy_loss_bwd": (i32, [P, vp, vp, vp, vp, vp, vp, vp, vp, i32, i32, vp, i32, vp, vp, vp]),
+        "sp_qk_norm_rope": (i32, [Q, vp, i64, vp, i64, vp, i64, vp, vp, vp, vp, vp, vp, vp]),
+        "sp_qk_workspace_size": (i32, [Q, ctypes.POINTER(sz)]),
+        "sp_qk_norm_rope_bwd": (i32, [Q, vp, i64, vp, i64, vp, vp, vp, vp, vp, vp, vp, i64, vp, i64, vp, i64, vp, vp,
+                                      vp, sz, vp]),
         "sp_attn_workspace_size": (i32, [D, i32, ctypes.POINTER(sz)]),
         "sp_attn_fwd": (i32, [D, vp, vp, vp, vp, vp, vp, sz, vp]),
         "sp_attn_fwd_static": (i32, [D, vp, vp, vp, vp, vp, vp]),
@@ -95,6 +119,8 @@ def load() -> ctypes.CDLL:
 
 EXPORTED = ["sp_status_string", "sp_version", "sp_ulysses_pack", "sp_ulysses_unpack",
             "sp_ulysses_unpack_add", "sp_token_logprob", "sp_token_logprob_bwd", "sp_loss_reduce",
+            "sp_policy_workspace_size", "sp_policy_loss", "sp_policy_loss_bwd",
+            "sp_qk_norm_rope", "sp_qk_workspace_size", "sp_qk_norm_rope_bwd",
             "sp_attn_workspace_size", "sp_attn_fwd", "sp_attn_fwd_static", "sp_attn_bwd", "sp_ring_step",
             "sp_lse_merge", "sp_f32_to_bf16", "sp_attn_schedule", "sp_attn_plan",
             "sp_profile_events"]
@@ -102,6 +128,7 @@ EXPORTED = ["sp_status_string", "sp_version", "sp_ulysses_pack", "sp_ulysses_unp
 SP_KERNEL_ATTN_FWD, SP_KERNEL_ATTN_DQ, SP_KERNEL_ATTN_DKDV = 1, 2, 3
 SP_KERNEL_PACK, SP_KERNEL_UNPACK, SP_KERNEL_LSE_MERGE, SP_KERNEL_UNPACK_ADD = 4, 5, 6, 7
 SP_KERNEL_TOKEN_LOGPROB, SP_KERNEL_TOKEN_LOGPROB_BWD = 8, 9
+SP_KERNEL_POLICY, SP_KERNEL_POLICY_BWD, SP_KERNEL_QK_ROPE, SP_KERNEL_QK_ROPE_BWD = 10, 11, 12, 13
 SP_LOSS_SFT, SP_LOSS_DPO = 0, 1
 
 
@@ -327,6 +354,204 @@ def sp_loss_reduce(partial_sums, kind: int, coef: float, ref_partial_sums=None, 
                                  float(coef), _ptr(loss), _ptr(grad), _stream(stream)),
            "sp_loss_reduce")
     return loss, grad
+
+
+def _device_of(stream) -> int:
+    import torch
+    return torch.cuda.current_device() if stream is None else stream.device.index
+
+
+def _arg(t, name: str, dtype, shape, device: int, optional: bool = False, rows: bool = False):
+    """Device pointer of a tensor argument.  The library reads memory by the
+    sizes it is told, so type, shape, device and layout are checked here
+    (`rows`: tokens may lie further apart than their heads need)."""
+    if t is None and optional:
+        return None
+    if t is None or t.dtype != dtype or tuple(t.shape) != shape:
+        raise ValueError(f"{name} must be a {dtype} tensor of shape {list(shape)}, got "
+                         + ("none" if t is None else f"{t.dtype} {list(t.shape)}"))
+    if not t.is_cuda or t.device.index != device:
+        raise ValueError(f"{name} must be on GPU {device}, where its stream is: it is on {t.device}")
+    if not (t[0].is_contiguous() if rows and shape[0] > 0 else t.is_contiguous()):
+        raise ValueError(f"{name} must be contiguous" + (" within a token" if rows else ""))
+    return t.data_ptr()
+
+
+class PolicyParams:
+    """The constants of a clipped policy loss (see include/sp_attn.h): a ratio
+    counts inside [1 - clip_low, 1 + clip_high]; advantages are [num_seqs] or,
+    with adv_per_token, [T]."""
+
+    def __init__(self, clip_low: float = 0.2, clip_high: float = 0.2, kl_coef: float = 0.0,
+                 entropy_coef: float = 0.0, adv_per_token: bool = False, ignore_index: int = -100):
+        self.c = SpPolicyParams(clip_low=clip_low, clip_high=clip_high, kl_coef=kl_coef, entropy_coef=entropy_coef,
+                                adv_per_token=1 if adv_per_token else 0, ignore_index=ignore_index)
+
+    @property
+    def ref(self):
+        return ctypes.byref(self.c)
+
+
+def sp_policy_workspace_size(T: int, V: int) -> int:
+    n = ctypes.c_size_t(0)
+    _check(load().sp_policy_workspace_size(T, V, ctypes.byref(n)), "sp_policy_workspace_size")
+    return n.value
+
+
+def _workspace(need: int, workspace, dev: int):
+    """The caller's workspace, or one allocated here if there is none or it is
+    too small."""
+    import torch
+    if workspace is not None and workspace.numel() * workspace.element_size() >= need:
+        if not workspace.is_cuda or workspace.device.index != dev or not workspace.is_contiguous():
+            raise ValueError(f"workspace must be contiguous on GPU {dev}")
+        return workspace
+    return torch.empty(need, dtype=torch.uint8, device=f"cuda:{dev}")
+
+
+def sp_policy_loss(params: PolicyParams, logits, labels, old_logp, ref_logp, advantages, cu_seqlens,
+                   with_entropy: bool = True, logp=None, lse=None, entropy=None, seq_sum=None, seq_stats=None,
+                   workspace=None, stream=None):
+    """logits [T, V] bf16, labels [T] int32, old_logp and ref_logp (or None) [T]
+    float32, advantages [num_seqs] or [T] float32 -> (logp, lse, entropy [T] --
+    None without entropy --, seq_sum [num_seqs], seq_stats [num_seqs, 4]: sums of
+    KL and entropy, clipped and counted tokens) float32."""
+    import torch
+    T, V = logits.shape
+    cu, cup, n = _cu(cu_seqlens)
+    n = max(n, 0)
+    f, dev = torch.float32, _device_of(stream)
+    per = T if params.c.adv_per_token else n
+    args = (_arg(logits, "logits", torch.bfloat16, (T, V), dev), _arg(labels, "labels", torch.int32, (T,), dev),
+            _arg(old_logp, "old_logp", f, (T,), dev), _arg(ref_logp, "ref_logp", f, (T,), dev, optional=True),
+            _arg(advantages, "advantages", f, (per,), dev))
+    with _alloc_on(stream):
+        def out(t, *shape):
+            return torch.empty(shape, dtype=f, device=logits.device) if t is None else t
+        logp, lse, seq_sum, seq_stats = out(logp, T), out(lse, T), out(seq_sum, n), out(seq_stats, n, 4)
+        if with_entropy:
+            entropy = out(entropy, T)
+        outs = (_arg(logp, "logp", f, (T,), dev), _arg(lse, "lse", f, (T,), dev),
+                _arg(entropy, "entropy", f, (T,), dev, optional=True), _arg(seq_sum, "seq_sum", f, (n,), dev),
+                _arg(seq_stats, "seq_stats", f, (n, 4), dev))
+        ws = _workspace(sp_policy_workspace_size(T, V), workspace, dev)
+        _check(load().sp_policy_loss(params.ref, *args, T, V, cup, n, *outs, ws.data_ptr(),
+                                     ws.numel() * ws.element_size(), _stream(stream)), "sp_policy_loss")
+    return logp, lse, entropy, seq_sum, seq_stats
+
+
+def sp_policy_loss_bwd(params: PolicyParams, logits, labels, logp, lse, entropy, old_logp, ref_logp, advantages,
+                       cu_seqlens, grad_seq, dlogits=None, stream=None):
+    """-> dlogits [T, V] bf16 (which may be the logits): the gradient of
+    sum(grad_seq * seq_sum), from what sp_policy_loss returned."""
+    import torch
+    T, V = logits.shape
+    cu, cup, n = _cu(cu_seqlens)
+    n = max(n, 0)
+    f, dev = torch.float32, _device_of(stream)
+    per = T if params.c.adv_per_token else n
+    args = (_arg(logits, "logits", torch.bfloat16, (T, V), dev), _arg(labels, "labels", torch.int32, (T,), dev),
+            _arg(logp, "logp", f, (T,), dev), _arg(lse, "lse", f, (T,), dev),
+            _arg(entropy, "entropy", f, (T,), dev, optional=True), _arg(old_logp, "old_logp", f, (T,), dev),
+            _arg(ref_logp, "ref_logp", f, (T,), dev, optional=True), _arg(advantages, "advantages", f, (per,), dev))
+    grad = _arg(grad_seq, "grad_seq", f, (n,), dev)
+    with _alloc_on(stream):
+        if dlogits is None:
+            dlogits = torch.empty_like(logits)
+        _check(load().sp_policy_loss_bwd(params.ref, *args, T, V, cup, n, grad,
+                                         _arg(dlogits, "dlogits", torch.bfloat16, (T, V), dev), _stream(stream)),
+               "sp_policy_loss_bwd")
+    return dlogits
+
+
+class QkDesc:
+    """Owns an sp_qk_desc and the host arrays it points to."""
+
+    def __init__(self, *, T, head_dim, H_q, H_kv, sp, q_map, kv_map, rotary_dim=None, inv_freq=None,
+                 interleaved=False, position_base=0, rope_scale=1.0, eps=1e-6, weight_offset=0.0):
+        qm, km = (np.ascontiguousarray(np.asarray(m, dtype=np.int32)) for m in (q_map, kv_map))
+        if sp < 1 or qm.size % sp or km.size % sp or not qm.size or not km.size:
+            raise ValueError("q_map and kv_map need the same number of slots for each of the sp ranks")
+        rot = (head_dim if rotary_dim is None else rotary_dim) if inv_freq is not None else (rotary_dim or 0)
+        f = np.ascontiguousarray(np.asarray([] if inv_freq is None else inv_freq, dtype=np.float64))
+        if f.size < rot // 2:
+            raise ValueError(f"inv_freq has fewer than {rot // 2} entries")
+        self._keep = (qm, km, f)
+        self.c = SpQkDesc(T=T, head_dim=head_dim, H_q=H_q, H_kv=H_kv, sp=sp, Hq_loc=qm.size // sp,
+                          Hkv_loc=km.size // sp, rotary_dim=rot, interleaved=1 if interleaved else 0,
+                          position_base=position_base, rope_scale=rope_scale, eps=eps, weight_offset=weight_offset,
+                          q_map=qm.ctypes.data_as(_i32p), kv_map=km.ctypes.data_as(_i32p),
+                          inv_freq=f.ctypes.data_as(ctypes.POINTER(ctypes.c_double)) if rot else None)
+
+    @property
+    def ref(self):
+        return ctypes.byref(self.c)
+
+
+def sp_qk_workspace_size(desc: QkDesc) -> int:
+    n = ctypes.c_size_t(0)
+    _check(load().sp_qk_workspace_size(desc.ref, ctypes.byref(n)), "sp_qk_workspace_size")
+    return n.value
+
+
+def _heads(t, name, shape, dev, optional=False):
+    """Pointer and token stride of a [T, H, D] bf16 tensor whose tokens may lie
+    further apart than their heads need."""
+    import torch
+    p = _arg(t, name, torch.bfloat16, shape, dev, optional=optional, rows=True)
+    return p, (shape[1] * shape[2] if t is None or shape[0] < 2 else t.stride(0))
+
+
+def sp_qk_norm_rope(desc: QkDesc, q, k, v, positions=None, w_q=None, w_k=None, q_dst=None, k_dst=None, v_dst=None,
+                    stream=None):
+    """q [T, H_q, D], k, v [T, H_kv, D] bf16 (any token stride) -> (q_dst [sp, T,
+    Hq_loc, D], k_dst, v_dst [sp, T, Hkv_loc, D]): normed (by w_q, w_k [D] bf16),
+    rotated by positions [T] int32 (None: position_base + t) and packed."""
+    import torch
+    c, dev, bf = desc.c, _device_of(stream), torch.bfloat16
+    T, D = c.T, c.head_dim
+    args = (*_heads(q, "q", (T, c.H_q, D), dev), *_heads(k, "k", (T, c.H_kv, D), dev),
+            *_heads(v, "v", (T, c.H_kv, D), dev), _arg(positions, "positions", torch.int32, (T,), dev, optional=True),
+            _arg(w_q, "w_q", bf, (D,), dev, optional=True), _arg(w_k, "w_k", bf, (D,), dev, optional=True))
+    sq, sk = (c.sp, T, c.Hq_loc, D), (c.sp, T, c.Hkv_loc, D)
+    with _alloc_on(stream):
+        q_dst, k_dst, v_dst = (torch.empty(s, dtype=bf, device=q.device) if t is None else t
+                               for t, s in ((q_dst, sq), (k_dst, sk), (v_dst, sk)))
+        _check(load().sp_qk_norm_rope(desc.ref, *args, _arg(q_dst, "q_dst", bf, sq, dev),
+                                      _arg(k_dst, "k_dst", bf, sk, dev), _arg(v_dst, "v_dst", bf, sk, dev),
+                                      _stream(stream)), "sp_qk_norm_rope")
+    return q_dst, k_dst, v_dst
+
+
+def sp_qk_norm_rope_bwd(desc: QkDesc, q, k, dq_src, dk_src, dv_src, positions=None, w_q=None, w_k=None, dq=None,
+                        dk=None, dv=None, dw_q=None, dw_k=None, workspace=None, stream=None):
+    """dq_src [sp, T, Hq_loc, D], dk_src, dv_src [sp, T, Hkv_loc, D] bf16 -> (dq
+    [T, H_q, D], dk, dv [T, H_kv, D] bf16, dw_q, dw_k [D] float32 -- None without
+    the weight).  q and k are needed where their weight is given."""
+    import torch
+    c, dev, bf, f = desc.c, _device_of(stream), torch.bfloat16, torch.float32
+    T, D = c.T, c.head_dim
+    sq, sk = (c.sp, T, c.Hq_loc, D), (c.sp, T, c.Hkv_loc, D)
+    hq, hk = (T, c.H_q, D), (T, c.H_kv, D)
+    args = (*_heads(q if w_q is not None else None, "q", hq, dev, optional=w_q is None),
+            *_heads(k if w_k is not None else None, "k", hk, dev, optional=w_k is None),
+            _arg(dq_src, "dq_src", bf, sq, dev), _arg(dk_src, "dk_src", bf, sk, dev),
+            _arg(dv_src, "dv_src", bf, sk, dev), _arg(positions, "positions", torch.int32, (T,), dev, optional=True),
+            _arg(w_q, "w_q", bf, (D,), dev, optional=True), _arg(w_k, "w_k", bf, (D,), dev, optional=True))
+    for w, dw, name in ((w_q, dw_q, "dw_q"), (w_k, dw_k, "dw_k")):
+        if w is None and dw is not None:
+            raise ValueError(f"{name} is given without its weight")
+    with _alloc_on(stream):
+        dq, dk, dv = (torch.empty(s, dtype=bf, device=dq_src.device) if t is None else t
+                      for t, s in ((dq, hq), (dk, hk), (dv, hk)))
+        dw_q, dw_k = (torch.empty(D, dtype=f, device=dq_src.device) if dw is None and w is not None else dw
+                      for w, dw in ((w_q, dw_q), (w_k, dw_k)))
+        ws = _workspace(sp_qk_workspace_size(desc), workspace, dev)
+        _check(load().sp_qk_norm_rope_bwd(desc.ref, *args, *_heads(dq, "dq", hq, dev), *_heads(dk, "dk", hk, dev),
+                                          *_heads(dv, "dv", hk, dev), _arg(dw_q, "dw_q", f, (D,), dev, optional=True),
+                                          _arg(dw_k, "dw_k", f, (D,), dev, optional=True), ws.data_ptr(),
+                                          ws.numel() * ws.element_size(), _stream(stream)), "sp_qk_norm_rope_bwd")
+    return dq, dk, dv, dw_q, dw_k
 
 
 def sp_attn_fwd(desc: Desc, q, k, v, o=None, lse=None, workspace=None, stream=None):

@@ -803,6 +803,185 @@ sp_status sp_loss_reduce(const float* partial_sums, const float* ref_partial_sum
   return SP_OK;
 }
 
+namespace {
+// Validation shared by the policy calls; fills the kernel arguments.
+sp_status policy_args(const sp_policy_params* p, int32_t T, int32_t V, const int32_t* cu, int32_t num_seqs,
+                      const float* ref_logp, const float* entropy, spk::LossArgs& a, spk::PolicyArgs& k) {
+  if (!p) return SP_ERR_INVALID_ARG;
+  sp_status st = loss_args(T, V, p->ignore_index, cu, num_seqs, a);
+  if (st != SP_OK) return st;
+  if (T >= 1 << 24) return SP_ERR_UNSUPPORTED;
+  if (!(p->clip_low >= 0.f && p->clip_low <= 1.f) || !(p->clip_high >= 0.f) || !std::isfinite(p->clip_high) ||
+      !std::isfinite(p->kl_coef) || !std::isfinite(p->entropy_coef) || (p->adv_per_token != 0 && p->adv_per_token != 1))
+    return SP_ERR_INVALID_ARG;
+  if ((!ref_logp && p->kl_coef != 0.f) || (!entropy && p->entropy_coef != 0.f)) return SP_ERR_INVALID_ARG;
+  k = spk::PolicyArgs{p->clip_low, p->clip_high, p->kl_coef, p->entropy_coef, p->adv_per_token, ref_logp != nullptr,
+                      entropy != nullptr, spk::policy_parts(T, V)};
+  return SP_OK;
+}
+size_t policy_workspace(int32_t T, int32_t V) {
+  return std::max<size_t>(256, align256((size_t)T * spk::policy_parts(T, V) * 16));
+}
+}  // namespace
+
+sp_status sp_policy_workspace_size(int32_t T, int32_t V, size_t* bytes) {
+  if (!bytes || T < 0 || V < 8 || V % 8 != 0) return SP_ERR_INVALID_ARG;
+  if (T >= 1 << 24) return SP_ERR_UNSUPPORTED;
+  *bytes = policy_workspace(T, V);
+  return SP_OK;
+}
+
+sp_status sp_policy_loss(const sp_policy_params* params, const void* logits, const int32_t* labels,
+                         const float* old_logp, const float* ref_logp, const float* advantages,
+                         int32_t T, int32_t V, const int32_t* cu_seqlens, int32_t num_seqs,
+                         float* logp, float* lse, float* entropy, float* seq_sum,
+                         float* seq_stats, void* workspace, size_t workspace_bytes, void* stream) {
+  spk::LossArgs a;
+  spk::PolicyArgs k;
+  sp_status st = policy_args(params, T, V, cu_seqlens, num_seqs, ref_logp, entropy, a, k);
+  if (st != SP_OK) return st;
+  if (T > 0 && (!logits || !labels || !old_logp || !logp || !lse || !aligned16(logits))) return SP_ERR_INVALID_ARG;
+  if (num_seqs > 0 && (!seq_sum || !seq_stats)) return SP_ERR_INVALID_ARG;
+  if (T > 0 && num_seqs > 0 && !advantages) return SP_ERR_INVALID_ARG;
+  if (!workspace || workspace_bytes < policy_workspace(T, V) || ((uintptr_t)workspace & 255u) != 0)
+    return SP_ERR_WORKSPACE;
+  const spk::PolicyTokens tok{labels, old_logp, ref_logp, advantages, logp, lse, entropy};
+  SP_HIP(spk::launch_policy_loss(a, k, logits, tok, workspace, seq_sum, seq_stats, (hipStream_t)stream));
+  return SP_OK;
+}
+
+sp_status sp_policy_loss_bwd(const sp_policy_params* params, const void* logits,
+                             const int32_t* labels, const float* logp, const float* lse,
+                             const float* entropy, const float* old_logp, const float* ref_logp,
+                             const float* advantages, int32_t T, int32_t V,
+                             const int32_t* cu_seqlens, int32_t num_seqs, const float* grad_seq,
+                             void* dlogits, void* stream) {
+  spk::LossArgs a;
+  spk::PolicyArgs k;
+  sp_status st = policy_args(params, T, V, cu_seqlens, num_seqs, ref_logp, entropy, a, k);
+  if (st != SP_OK) return st;
+  if (T == 0) return SP_OK;
+  if (!logits || !labels || !logp || !lse || !old_logp || !dlogits || !aligned16(logits) || !aligned16(dlogits) ||
+      (num_seqs > 0 && (!grad_seq || !advantages)))
+    return SP_ERR_INVALID_ARG;
+  const spk::PolicyTokens tok{labels, old_logp, ref_logp, advantages, const_cast<float*>(logp), const_cast<float*>(lse),
+                              const_cast<float*>(entropy)};
+  SP_HIP(spk::launch_policy_loss_bwd(a, k, logits, tok, grad_seq, dlogits, (hipStream_t)stream));
+  return SP_OK;
+}
+
+namespace {
+// Validation of a sp_qk_desc; fills the forward's kernel arguments.
+sp_status qk_args(const sp_qk_desc* d, spk::QkArgs& a) {
+  if (!d) return SP_ERR_INVALID_ARG;
+  if (d->T < 0 || d->H_q < 1 || d->H_kv < 1 || d->sp < 1 || d->Hq_loc < 1 || d->Hkv_loc < 1 || d->rotary_dim < 0 ||
+      (d->interleaved != 0 && d->interleaved != 1) || !d->q_map || !d->kv_map || (d->rotary_dim > 0 && !d->inv_freq))
+    return SP_ERR_INVALID_ARG;
+  if (d->head_dim != 64 && d->head_dim != 128) return SP_ERR_UNSUPPORTED;
+  if (d->rotary_dim % 16 != 0 || d->rotary_dim > d->head_dim) return SP_ERR_INVALID_ARG;
+  if (!std::isfinite(d->rope_scale) || !std::isfinite(d->weight_offset) || !(d->eps >= 0.f) || !std::isfinite(d->eps))
+    return SP_ERR_INVALID_ARG;
+  if ((int64_t)d->sp * d->Hq_loc > spk::kMaxMap || (int64_t)d->sp * d->Hkv_loc > spk::kMaxMap ||
+      d->H_q > spk::kMaxQkHeads || d->H_kv > spk::kMaxQkHeads || d->T >= 1 << 24)
+    return SP_ERR_UNSUPPORTED;
+  a.T = d->T; a.Hq = d->H_q; a.Hkv = d->H_kv; a.sp = d->sp; a.Hq_loc = d->Hq_loc; a.Hkv_loc = d->Hkv_loc;
+  a.rot = d->rotary_dim; a.neigh = d->interleaved; a.pos_base = d->position_base;
+  a.rope_scale = d->rope_scale; a.eps = d->eps; a.w_off = d->weight_offset;
+  for (int i = 0; i < d->rotary_dim / 2; ++i) {
+    if (!std::isfinite(d->inv_freq[i])) return SP_ERR_INVALID_ARG;
+    // the fraction of a turn, in 2^-64: the long double has 64 bits for it
+    const long double turns = (long double)d->inv_freq[i] / 6.283185307179586476925286766559L;
+    const long double frac = turns - floorl(turns);
+    const long double fixed = roundl(frac * 18446744073709551616.0L);
+    a.freq[i] = fixed >= 18446744073709551616.0L ? 0 : (uint64_t)fixed;
+  }
+  auto entries = [&](const int32_t* map, int H_loc, int H, uint32_t* slot) {
+    for (int i = 0; i < d->sp * H_loc; ++i) {
+      if (map[i] < -1 || map[i] >= H) return false;
+      slot[i] = (uint32_t)(i % H_loc) | (uint32_t)(i / H_loc) << 10 | (uint32_t)(map[i] + 1) << 20;
+    }
+    return true;
+  };
+  if (!entries(d->q_map, d->Hq_loc, d->H_q, a.q_slot) || !entries(d->kv_map, d->Hkv_loc, d->H_kv, a.kv_slot))
+    return SP_ERR_INVALID_ARG;
+  return SP_OK;
+}
+// The entries of every head, ascending, in `slot` (which holds them by slot).
+void by_head(uint32_t* slot, int n, int H, int16_t* start) {
+  uint32_t sorted[spk::kMaxMap];
+  int at = 0;
+  for (int g = 0; g <= H; ++g) start[g] = 0;
+  for (int i = 0; i < n; ++i)
+    if (slot[i] >> 20) ++start[slot[i] >> 20];
+  for (int g = 0; g < H; ++g) start[g + 1] += start[g];
+  int16_t next[spk::kMaxQkHeads];
+  std::copy(start, start + H, next);
+  for (int i = 0; i < n; ++i)
+    if (slot[i] >> 20) sorted[next[(slot[i] >> 20) - 1]++] = slot[i], ++at;
+  std::copy(sorted, sorted + at, slot);
+}
+bool qk_stride_ok(const sp_qk_desc* d, int64_t stride, int H) {
+  return stride % 8 == 0 && stride >= (int64_t)H * d->head_dim && stride < (int64_t(1) << 40);
+}
+size_t qk_workspace(const sp_qk_desc* d) {
+  return align256((size_t)spk::qk_bwd_groups(d->T) * 2 * d->head_dim * sizeof(float));
+}
+}  // namespace
+
+sp_status sp_qk_norm_rope(const sp_qk_desc* d, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                          const void* v, int64_t v_stride, const int32_t* positions, const void* w_q, const void* w_k,
+                          void* q_dst, void* k_dst, void* v_dst, void* stream) {
+  spk::QkArgs a{};
+  sp_status s = qk_args(d, a);
+  if (s != SP_OK) return s;
+  if (!qk_stride_ok(d, q_stride, d->H_q) || !qk_stride_ok(d, k_stride, d->H_kv) || !qk_stride_ok(d, v_stride, d->H_kv))
+    return SP_ERR_INVALID_ARG;
+  if (d->T == 0) return SP_OK;
+  for (const void* ptr : {q, k, v, (const void*)q_dst, (const void*)k_dst, (const void*)v_dst})
+    if (!ptr || !aligned16(ptr)) return SP_ERR_INVALID_ARG;
+  if (!aligned16(w_q) || !aligned16(w_k)) return SP_ERR_INVALID_ARG;
+  a.sq = q_stride / 8; a.sk = k_stride / 8; a.sv = v_stride / 8;
+  SP_HIP(spk::launch_qk_rope(a, d->head_dim, q, k, v, positions, w_q, w_k, q_dst, k_dst, v_dst, (hipStream_t)stream));
+  return SP_OK;
+}
+
+sp_status sp_qk_workspace_size(const sp_qk_desc* d, size_t* bytes) {
+  if (!bytes) return SP_ERR_INVALID_ARG;
+  spk::QkArgs a;
+  sp_status s = qk_args(d, a);
+  if (s != SP_OK) return s;
+  *bytes = qk_workspace(d);
+  return SP_OK;
+}
+
+sp_status sp_qk_norm_rope_bwd(const sp_qk_desc* d, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                              const void* dq_src, const void* dk_src, const void* dv_src, const int32_t* positions,
+                              const void* w_q, const void* w_k, void* dq, int64_t dq_stride, void* dk, int64_t dk_stride,
+                              void* dv, int64_t dv_stride, float* dw_q, float* dw_k, void* ws, size_t ws_bytes,
+                              void* stream) {
+  spk::QkBwdArgs b{};
+  sp_status s = qk_args(d, b.a);
+  if (s != SP_OK) return s;
+  if (!qk_stride_ok(d, dq_stride, d->H_q) || !qk_stride_ok(d, dk_stride, d->H_kv) || !qk_stride_ok(d, dv_stride, d->H_kv) ||
+      (w_q && !qk_stride_ok(d, q_stride, d->H_q)) || (w_k && !qk_stride_ok(d, k_stride, d->H_kv)))
+    return SP_ERR_INVALID_ARG;
+  if (!w_q != !dw_q || !w_k != !dw_k) return SP_ERR_INVALID_ARG;
+  if (d->T > 0) {
+    for (const void* ptr : {dq_src, dk_src, dv_src, (const void*)dq, (const void*)dk, (const void*)dv})
+      if (!ptr || !aligned16(ptr)) return SP_ERR_INVALID_ARG;
+    if ((w_q && !q) || (w_k && !k)) return SP_ERR_INVALID_ARG;
+    if (!aligned16(q) || !aligned16(k) || !aligned16(w_q) || !aligned16(w_k)) return SP_ERR_INVALID_ARG;
+  }
+  if (!ws || ws_bytes < qk_workspace(d) || ((uintptr_t)ws & 255u) != 0) return SP_ERR_WORKSPACE;
+  b.a.sq = q_stride / 8; b.a.sk = k_stride / 8;
+  b.dsq = dq_stride / 8; b.dsk = dk_stride / 8; b.dsv = dv_stride / 8;
+  by_head(b.a.q_slot, d->sp * d->Hq_loc, d->H_q, b.q_start);
+  by_head(b.a.kv_slot, d->sp * d->Hkv_loc, d->H_kv, b.kv_start);
+  SP_HIP(spk::launch_qk_rope_bwd(b, d->head_dim, q, k, dq_src, dk_src, dv_src, positions, w_q, w_k, dq, dk, dv, dw_q, dw_k,
+                                 w_q || w_k ? (float*)ws : nullptr, (hipStream_t)stream));
+  return SP_OK;
+}
+
 sp_status sp_attn_workspace_size(const sp_attn_desc* desc, int32_t op, size_t* bytes) {
   if (!bytes) return SP_ERR_INVALID_ARG;
   if (op != SP_OP_FWD && op != SP_OP_BWD && op != SP_OP_RING_STEP) return SP_ERR_INVALID_ARG;

@@ -9,7 +9,7 @@ namespace spk {
 // SP_KERNEL_* constants of the public header).
 enum KernelId {
   kKFwd = 1, kKDq = 2, kKDkdv = 3, kKPack = 4, kKUnpack = 5, kKMerge = 6, kKUnpackAdd = 7,
-  kKLogprob = 8, kKLogprobBwd = 9, kKCount = 10
+  kKLogprob = 8, kKLogprobBwd = 9, kKPolicy = 10, kKPolicyBwd = 11, kKQkRope = 12, kKQkRopeBwd = 13, kKCount = 14
 };
 
 struct KernelTimer {
@@ -88,6 +88,37 @@ struct LossArgs {
 struct LossReduceArgs {
   int sp, n, kind;  // kind 0 = SFT, 1 = DPO
   float coef;       // SFT: loss scale; DPO: beta
+};
+
+// Policy loss: the parameters of sp_policy_params, whether there is a reference
+// model, whether the entropy is formed, and the parts a row is split in.
+struct PolicyArgs {
+  float clip_low, clip_high, kl_coef, entropy_coef;
+  int adv_per_token, has_ref, entropy, parts;
+};
+// Per-token arrays [T] (adv: [T] or [n_seqs]); logp, lse and ent are written by
+// the forward and read by the backward.
+struct PolicyTokens {
+  const int32_t* labels;
+  const float *old_logp, *ref_logp, *adv;
+  float *logp, *lse, *ent;
+};
+
+// Norm, rotation and pack of query / key heads.  A slot entry: slot of its rank in
+// bits 0-9, rank in bits 10-19, head + 1 (0: a dummy) above.  Strides in 16-byte
+// chunks a token; frequencies in 2^-64 turns a position.
+static constexpr int kMaxQkHeads = 256;
+struct QkArgs {
+  int T, Hq, Hkv, sp, Hq_loc, Hkv_loc, rot, neigh, pos_base;
+  float rope_scale, eps, w_off;
+  int64_t sq, sk, sv;
+  uint64_t freq[64];
+  uint32_t q_slot[kMaxMap], kv_slot[kMaxMap];  // forward: by slot; backward: by head, ascending
+};
+struct QkBwdArgs {
+  QkArgs a;
+  int64_t dsq, dsk, dsv;
+  int16_t q_start[kMaxQkHeads + 1], kv_start[kMaxQkHeads + 1];  // a head's entries
 };
 
 struct ReduceArgs {
@@ -185,6 +216,18 @@ hipError_t launch_token_logprob_bwd(const LossArgs& a, const void* logits, const
                                     hipStream_t st);
 hipError_t launch_loss_reduce(const LossReduceArgs& a, const float* ps, const float* refs,
                               float* loss, float* grad, hipStream_t st);
+int policy_parts(int T, int V);
+hipError_t launch_policy_loss(const LossArgs& a, const PolicyArgs& p, const void* logits, const PolicyTokens& tok,
+                              void* part, float* seq_sum, float* stats, hipStream_t st);
+hipError_t launch_policy_loss_bwd(const LossArgs& a, const PolicyArgs& p, const void* logits, const PolicyTokens& tok,
+                                  const float* grad_seq, void* dlogits, hipStream_t st);
+int qk_bwd_groups(int T);
+hipError_t launch_qk_rope(const QkArgs& a, int D, const void* q, const void* k, const void* v, const int32_t* positions,
+                          const void* w_q, const void* w_k, void* q_dst, void* k_dst, void* v_dst, hipStream_t st);
+hipError_t launch_qk_rope_bwd(const QkBwdArgs& b, int D, const void* q, const void* k, const void* dq_src,
+                              const void* dk_src, const void* dv_src, const int32_t* positions, const void* w_q,
+                              const void* w_k, void* dq, void* dk, void* dv, float* dw_q, float* dw_k, float* part,
+                              hipStream_t st);
 hipError_t launch_merge(float* o_acc, float* lse_acc, const void* o_part, bool part_bf16,
                         const float* lse_part, int T, int H, int D, void* o_out, hipStream_t st);
 hipError_t launch_zero_heads_bf16(void* x, int T, int H, int D, int h0, int h1, hipStream_t st);
