@@ -150,6 +150,25 @@ enum { SP_OP_FWD = 0, SP_OP_BWD = 1, SP_OP_RING_STEP = 2 };
  */
 #define SP_DESC_DQ_ACC_INIT 8
 
+/*
+ * SP_DESC_SHARED_PREFIX: segments that share a prefix, which is in the batch once
+ * -- a prompt and several answers to it, packed [prompt | answer | answer | ...]
+ * with the answers' position_ids continuing the prompt's.  prefix_of[s] (HOST,
+ * num_seqs entries, read only under this flag) is -1, or the segment whose keys,
+ * all of them and whatever their positions, the rows of segment s see next to
+ * their own segment's as always.  A prefix has none itself, and the segments that
+ * share it follow it at once, one after the other: prefix_of[s] is -1, or s - 1,
+ * or prefix_of[s - 1]; under causal = 1 a prefix with rows shows its last row all
+ * its keys (else SP_ERR_INVALID_ARG).  A prefix without rows is one whose keys alone
+ * are there.  The outputs and gradients are those of the unpacked sequences
+ * [prompt, answer] with the prompt's rows counted once: dk and dv of its keys sum
+ * over its own rows and every answer's.  Supported by sp_attn_fwd,
+ * sp_attn_fwd_static, sp_attn_bwd, sp_attn_workspace_size, sp_attn_schedule and
+ * sp_attn_plan; sp_ring_step and SP_OP_RING_STEP return SP_ERR_UNSUPPORTED, and
+ * SP_DESC_SINGLE_SEQUENCE beside it SP_ERR_INVALID_ARG.
+ */
+#define SP_DESC_SHARED_PREFIX 32
+
 typedef struct sp_attn_desc {
   int32_t T_q;              /* query tokens at this rank (rows of q, o, dq)         */
   int32_t T_k;              /* key tokens (rows of k, v, dk, dv)                     */
@@ -169,6 +188,7 @@ typedef struct sp_attn_desc {
   const int32_t* cu_seqlens_k;   /* HOST, num_seqs + 1                               */
   const int32_t* position_ids_q; /* HOST, T_q, or NULL                               */
   const int32_t* position_ids_k; /* HOST, T_k, or NULL                               */
+  const int32_t* prefix_of;      /* HOST, num_seqs; read under SP_DESC_SHARED_PREFIX */
 } sp_attn_desc;
 
 /* Human-readable name of a status code (static storage). */
@@ -366,6 +386,9 @@ sp_status sp_f32_to_bf16(const float* src, void* dst, int64_t n, void* stream);
  *       key <= row + delta.  Row tiles hold 256 rows; under a causal mask
  *       they end at the segment's end, so a partial tile is the segment's
  *       first (its rows see the fewest keys).
+ *       With SP_DESC_SHARED_PREFIX a row item holds up to eight groups of at most
+ *       32 rows of segments that share a prefix; it is listed as one such entry a
+ *       group, and one more with its prefix's keys and delta = 2^30.
  *   SP_OP_BWD, dK/dV items: {k_begin, k_end, q_begin, q_end, delta, head,
  *       kv_head, 1}.
  * A launch of few items splits each of them over S workgroups (row items: S =

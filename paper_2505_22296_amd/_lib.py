@@ -23,6 +23,7 @@ SP_OP_FWD, SP_OP_BWD, SP_OP_RING_STEP = 0, 1, 2
 SP_DESC_SINGLE_SEQUENCE = 1
 SP_DESC_ROWSTATS_READY = 4
 SP_DESC_DQ_ACC_INIT = 8
+SP_DESC_SHARED_PREFIX = 32
 SCHED_ITEM_INTS = 8
 PLAN_INTS = 6
 
@@ -39,7 +40,7 @@ class SpAttnDesc(ctypes.Structure):
         ("causal", ctypes.c_int32), ("softmax_scale", ctypes.c_float),
         ("flags", ctypes.c_int32),
         ("cu_seqlens_q", _i32p), ("cu_seqlens_k", _i32p),
-        ("position_ids_q", _i32p), ("position_ids_k", _i32p),
+        ("position_ids_q", _i32p), ("position_ids_k", _i32p), ("prefix_of", _i32p),
     ]
 
 
@@ -148,7 +149,7 @@ class Desc:
                  num_padded_heads, gqa_group, Hkv_loc, kv_head_offset, cu_seqlens_q,
                  cu_seqlens_k, position_ids_q=None, position_ids_k=None, causal=True,
                  softmax_scale=None, single_sequence=False, rowstats_ready=False,
-                 dq_acc_init=False):
+                 dq_acc_init=False, prefix_of=None):
         self._keep = []
 
         def arr(x):
@@ -166,6 +167,8 @@ class Desc:
                              ("position_ids_k", position_ids_k, T_k)):
             if pos is not None and len(np.asarray(pos)) < T:
                 raise ValueError(f"{name} has fewer than {T} entries")
+        if prefix_of is not None and len(np.asarray(prefix_of)) != max(0, len(cq) - 1):
+            raise ValueError("prefix_of needs one entry per segment")
         self.c = SpAttnDesc(
             T_q=T_q, T_k=T_k, head_dim=head_dim, H_loc=H_loc, head_offset=head_offset,
             num_real_heads=num_real_heads, num_padded_heads=num_padded_heads,
@@ -174,9 +177,11 @@ class Desc:
             softmax_scale=(1.0 / math.sqrt(head_dim)) if softmax_scale is None else softmax_scale,
             flags=((SP_DESC_SINGLE_SEQUENCE if single_sequence else 0)
                    | (SP_DESC_ROWSTATS_READY if rowstats_ready else 0)
-                   | (SP_DESC_DQ_ACC_INIT if dq_acc_init else 0)),
+                   | (SP_DESC_DQ_ACC_INIT if dq_acc_init else 0)
+                   | (SP_DESC_SHARED_PREFIX if prefix_of is not None else 0)),
             cu_seqlens_q=arr(cu_seqlens_q), cu_seqlens_k=arr(cu_seqlens_k),
-            position_ids_q=arr(position_ids_q), position_ids_k=arr(position_ids_k))
+            position_ids_q=arr(position_ids_q), position_ids_k=arr(position_ids_k),
+            prefix_of=arr(prefix_of))
 
     @property
     def ref(self):

@@ -50,6 +50,9 @@ struct Problem {
   std::vector<int> kv_of;    // per real local head
   std::vector<int> kv_lo, kv_hi;  // per local KV head: real heads [lo, hi) reading it
   bool direct = true;        // every KV head read by at most one real local head
+  // SP_DESC_SHARED_PREFIX: per segment, the segment whose keys it sees too (-1:
+  // none); empty without the flag.
+  std::vector<int> prefix;
 };
 
 
@@ -106,6 +109,33 @@ sp_status single_sequence_runs(const sp_attn_desc* d, Problem& p) {
   return SP_OK;
 }
 
+// Shared prefixes (SP_DESC_SHARED_PREFIX).  The segments that share a prefix
+// follow it, so the rows that see a prefix's keys are its own and then, to the
+// group's end, every row: one range, for which the prefix's causal rule also holds
+// behind its rows, as its last row sees all its keys.  Row tiles are another
+// matter (RowTiles).
+sp_status shared_prefixes(const sp_attn_desc* d, Problem& p) {
+  const int n = d->num_seqs;
+  if (n > 0 && !d->prefix_of) return SP_ERR_INVALID_ARG;
+  p.prefix.assign(d->prefix_of, d->prefix_of + n);
+  for (int s = 0; s < n; ++s) {
+    const int f = p.prefix[s];
+    if (f < -1 || f >= s) return SP_ERR_INVALID_ARG;
+    if (f < 0) continue;
+    if (p.prefix[f] != -1 || (f != s - 1 && p.prefix[s - 1] != f)) return SP_ERR_INVALID_ARG;
+    Seg& k = p.segs_k[f];
+    const Seg& own = p.segs[f];
+    if (own.qb == own.qa)
+      k.delta = own.kb - own.qa;  // no rows of its own: every row of the group sees every key
+    else if (d->causal && (int64_t)own.delta < (int64_t)own.kb - own.qb)
+      return SP_ERR_INVALID_ARG;
+    k.qb = p.segs[s].qb;
+  }
+  // nothing shared: separate segments as ever
+  if (std::all_of(p.prefix.begin(), p.prefix.end(), [](int f) { return f < 0; })) p.prefix.clear();
+  return SP_OK;
+}
+
 // The O(T) checks that every segment's positions form a +1 ramp run unless
 // the environment sets SPATTN_VALIDATE=0 (read once per process); without
 // them only each segment's first position is read, and a malformed ramp
@@ -120,9 +150,11 @@ bool ramp_checks() {
 
 sp_status validate(const sp_attn_desc* d, Problem& p) {
   if (!d) return SP_ERR_INVALID_ARG;
-  if (d->flags & ~(SP_DESC_SINGLE_SEQUENCE | SP_DESC_ROWSTATS_READY | SP_DESC_DQ_ACC_INIT))
+  if (d->flags & ~(SP_DESC_SINGLE_SEQUENCE | SP_DESC_ROWSTATS_READY | SP_DESC_DQ_ACC_INIT | SP_DESC_SHARED_PREFIX))
     return SP_ERR_INVALID_ARG;
   const bool single = (d->flags & SP_DESC_SINGLE_SEQUENCE) != 0;
+  const bool shared = (d->flags & SP_DESC_SHARED_PREFIX) != 0;
+  if (single && shared) return SP_ERR_INVALID_ARG;
   if (d->T_q < 0 || d->T_k < 0 || d->T_q >= kMaxTokens || d->T_k >= kMaxTokens)
     return SP_ERR_INVALID_ARG;
   if (d->head_dim != 64 && d->head_dim != 128) return SP_ERR_UNSUPPORTED;
@@ -201,6 +233,7 @@ sp_status validate(const sp_attn_desc* d, Problem& p) {
   }
   p.segs_k = p.segs;
   if (single) return single_sequence_runs(d, p);
+  if (shared) return shared_prefixes(d, p);
   return SP_OK;
 }
 
@@ -473,6 +506,151 @@ Costs schedule_rows(const sp_attn_desc* d, const Problem& p, int BM, int BN, boo
   return costs_of(items);
 }
 
+// Row tiles of a batch with shared prefixes: eight slots of up to 32 rows.  A slot
+// holds rows of one segment; the slots of a tile share a prefix, whose keys the
+// tile walks once for all of them, and then what they see of their own segments.
+// A segment's full tiles are 256 rows at its end (causal: the rest are its first
+// rows, which see the fewest keys); the rests of all segments of one prefix are
+// put into tiles together (16 answers of 600 rows to a prompt of 8192: 42 tiles a
+// head instead of 53).  Segments without a prefix are tiled one by one as ever.
+struct RowTile {
+  std::vector<spk::RowSlot> slots;  // at most 8
+  int prefix = -1;                  // a segment
+};
+constexpr int kSlotRows = 32, kSlots = 8;
+static_assert(spk::kFwdBM == kSlotRows * kSlots && spk::kDqBM == kSlotRows * kSlots, "slots of a row tile");
+
+std::vector<RowTile> row_tiles(const sp_attn_desc* d, const Problem& p) {
+  std::vector<RowTile> tiles;
+  auto cut = [&](RowTile& t, const Seg& g, int a, int b) {  // rows [a, b), at most one tile's
+    for (; a < b; a += kSlotRows)
+      t.slots.push_back({a, std::min(a + kSlotRows, b), g.ka, g.kb, g.delta});
+  };
+  std::vector<spk::RowSlot> open;  // rests of segments of prefix `of`
+  int of = -1;
+  auto flush = [&] {
+    for (size_t i = 0; i < open.size(); i += kSlots)
+      tiles.push_back({{open.begin() + i, open.begin() + std::min(open.size(), i + kSlots)}, of});
+    open.clear();
+  };
+  for (size_t s = 0; s < p.segs.size(); ++s) {
+    const Seg& g = p.segs[s];
+    const int BM = kSlotRows * kSlots, part = (g.qb - g.qa) % BM;
+    const int f0 = d->causal ? g.qa + part : g.qa, f1 = d->causal ? g.qb : g.qb - part;  // full tiles
+    const int r0 = d->causal ? g.qa : f1, r1 = d->causal ? f0 : g.qb;                    // the rest
+    if (p.prefix[s] != of) {
+      flush();
+      of = p.prefix[s];
+    }
+    RowTile t;
+    cut(t, g, r0, r1);
+    if (of >= 0) {
+      open.insert(open.end(), t.slots.begin(), t.slots.end());
+    } else if (r1 > r0) {
+      tiles.push_back(t);
+    }
+    for (int a = f0; a < f1; a += BM) {
+      tiles.push_back({{}, of});
+      cut(tiles.back(), g, a, a + BM);
+    }
+  }
+  flush();
+  const Seg pad{p.q_pad, d->T_q, 0, 0, 0};
+  for (int a = pad.qa; a < pad.qb; a += kSlotRows * kSlots) {
+    tiles.push_back({{}, -1});
+    cut(tiles.back(), pad, a, std::min(a + kSlotRows * kSlots, pad.qb));
+  }
+  return tiles;
+}
+
+// Own keys [first, second) that a slot sees some of.
+std::pair<int, int> own_keys(const sp_attn_desc* d, const spk::RowSlot& s) {
+  const int k1 = d->causal ? (int)std::min<int64_t>(s.k1, (int64_t)s.row1 + s.delta) : s.k1;
+  return {s.k0, std::max(s.k0, k1)};
+}
+
+// Key tiles of BN keys of the slots [a, b) of a tile; with `record`, their record
+// (layout: RowSlot in dev_common.h) for a workgroup of n slots.
+int slot_record(const sp_attn_desc* d, const Problem& p, const RowTile& t, size_t a, size_t b, int BN, int n,
+                int32_t* record) {
+  std::vector<std::pair<int, int>> own;
+  for (size_t i = a; i < b; ++i) {
+    const auto k = own_keys(d, t.slots[i]);
+    if (k.second <= k.first) continue;
+    // (slots ascend: ranges that meet or overlap are one)
+    if (!own.empty() && k.first <= own.back().second)
+      own.back().second = std::max(own.back().second, k.second);
+    else
+      own.push_back(k);
+  }
+  int tiles = 0, r = 0;
+  auto range = [&](int k0, int k1) {
+    const int first = k0 & ~7;
+    tiles += (k1 - first + BN - 1) / BN;
+    if (record) {
+      int32_t* o = record + spk::kRecordRanges + 3 * r++;
+      o[0] = tiles;
+      o[1] = first;
+      o[2] = k1;
+    }
+  };
+  // (rows that do not exist see no prefix either)
+  const bool prefix = t.prefix >= 0 && b > a && p.segs[t.prefix].kb > p.segs[t.prefix].ka;
+  if (prefix) range(p.segs[t.prefix].ka, p.segs[t.prefix].kb);
+  for (const auto& k : own) range(k.first, k.second);
+  if (record) {
+    record[0] = tiles;
+    record[1] = prefix ? p.segs[t.prefix].ka : 0;
+    record[2] = prefix;
+    int32_t* o = record + spk::kRecordRanges + 3 * (1 + n);
+    for (size_t i = a; i < b; ++i, o += 5) {
+      const spk::RowSlot& s = t.slots[i];
+      o[0] = s.row0; o[1] = s.row1; o[2] = s.k0; o[3] = s.k1; o[4] = s.delta;
+    }
+  }
+  return tiles;
+}
+
+// Row items over such tiles; an item's first field is its tile's number until
+// place_records puts the records' place there.  Returns their steps, longest first.
+Costs schedule_tiles(const sp_attn_desc* d, const Problem& p, const std::vector<RowTile>& tiles, int BN,
+                     std::vector<int32_t>& out, size_t n_front) {
+  std::vector<Item> items;
+  std::vector<int> steps;
+  for (const RowTile& t : tiles) steps.push_back(slot_record(d, p, t, 0, t.slots.size(), BN, kSlots, nullptr));
+  for (int y = 0; y < p.n_real; ++y)
+    for (size_t i = 0; i < tiles.size(); ++i)
+      items.push_back(Item{{(int)i, 0, 0, 0, 0, y, p.kv_of[y], 0}, steps[i]});
+  sort_items(items, out, n_front, true);
+  return costs_of(items);
+}
+
+// The records of every tile for launches that split its rows over `split`
+// workgroups; the items' first fields, from item `front` on, become the records'
+// places in a list where they start at int `base`.
+std::vector<int32_t> place_records(const sp_attn_desc* d, const Problem& p, const std::vector<RowTile>& tiles, int split,
+                                   int BN, std::vector<int32_t>& items, size_t front, int base) {
+  const int n = kSlots / split, ints = spk::record_ints(n);
+  std::vector<int32_t> out((size_t)ints * split * tiles.size(), 0);
+  for (size_t i = 0; i < tiles.size(); ++i)
+    for (int w = 0; w < split; ++w) {
+      const size_t a = std::min<size_t>(tiles[i].slots.size(), (size_t)w * n);
+      const size_t b = std::min<size_t>(tiles[i].slots.size(), a + n);
+      slot_record(d, p, tiles[i], a, b, BN, n, &out[(i * split + w) * ints]);
+    }
+  for (size_t i = front; i < items.size() / kItemInts; ++i)
+    items[i * kItemInts] = base + items[i * kItemInts] * split * ints;
+  return out;
+}
+// Either kind of row items.
+Costs schedule_row_items(const sp_attn_desc* d, const Problem& p, const std::vector<RowTile>& tiles, int BM, int BN,
+                         bool include_empty, std::vector<int32_t>& out, size_t n_front) {
+  return p.prefix.empty() ? schedule_rows(d, p, BM, BN, include_empty, out, n_front)
+                          : schedule_tiles(d, p, tiles, BN, out, n_front);
+}
+// Ints of the records under any split.
+size_t record_room(size_t n_tiles) { return n_tiles * 4 * (size_t)spk::record_ints(kSlots / 4); }
+
 // Key-tile items (dK / dV).  Every key of every real head gets exactly one
 // item.  Returns their steps, longest first.
 Costs schedule_keys(const sp_attn_desc* d, const Problem& p, int BNK, int BQ,
@@ -577,11 +755,15 @@ Layout layout_for(const sp_attn_desc* d, const Problem& p, int op, size_t n_item
 // the workspace is sized for) and of schedule_keys, without building them.
 // (With the zero-fill items appended at launch.)
 size_t row_item_count(const sp_attn_desc* d, const Problem& p, int BM) {
+  const size_t fills =
+      (size_t)(d->H_loc - p.n_real) * (size_t)((d->T_q + spk::kFillRows - 1) / spk::kFillRows);
+  if (!p.prefix.empty()) {  // the records lie behind the items
+    const size_t tiles = row_tiles(d, p).size();
+    return tiles * (size_t)p.n_real + fills + record_room(tiles) / kItemInts;
+  }
   size_t per_head = 0;
   for (const Seg& g : p.segs) per_head += (size_t)((g.qb - g.qa) + BM - 1) / BM;
   per_head += (size_t)((d->T_q - p.q_pad) + BM - 1) / BM;
-  const size_t fills =
-      (size_t)(d->H_loc - p.n_real) * (size_t)((d->T_q + spk::kFillRows - 1) / spk::kFillRows);
   return per_head * (size_t)p.n_real + fills;
 }
 size_t key_item_count(const sp_attn_desc* d, const Problem& p, int BNK) {
@@ -988,6 +1170,7 @@ sp_status sp_attn_workspace_size(const sp_attn_desc* desc, int32_t op, size_t* b
   Problem p;
   sp_status s = validate(desc, p);
   if (s != SP_OK) return s;
+  if (op == SP_OP_RING_STEP && !p.prefix.empty()) return SP_ERR_UNSUPPORTED;
   size_t a = 0, b = 0;
   item_counts(desc, p, op, a, b);
   *bytes = layout_for(desc, p, op, a, b).total;
@@ -1003,7 +1186,21 @@ sp_status sp_attn_schedule(const sp_attn_desc* desc, int32_t op, int32_t* items,
   std::vector<int32_t> v;
   // in launch order: the fill items that precede the listed ones there
   // shift the workgroup -> XCD map
-  if (op == SP_OP_FWD || op == SP_OP_RING_STEP)
+  if ((op == SP_OP_FWD || op == SP_OP_RING_STEP) && !p.prefix.empty()) {
+    if (op == SP_OP_RING_STEP) return SP_ERR_UNSUPPORTED;
+    const std::vector<RowTile> tiles = row_tiles(desc, p);
+    std::vector<int32_t> it;
+    schedule_tiles(desc, p, tiles, spk::kFwdBN, it, row_fills(desc, p).size() / kItemInts);
+    for (size_t i = 0; i < it.size(); i += kItemInts) {  // slot by slot
+      const RowTile& t = tiles[it[i]];
+      for (const spk::RowSlot& s : t.slots) {
+        const auto own = own_keys(desc, s);
+        v.insert(v.end(), {s.row0, s.row1, own.first, own.second, s.delta, it[i + 5], it[i + 6], 0});
+        if (t.prefix >= 0)
+          v.insert(v.end(), {s.row0, s.row1, p.segs[t.prefix].ka, p.segs[t.prefix].kb, 1 << 30, it[i + 5], it[i + 6], 0});
+      }
+    }
+  } else if (op == SP_OP_FWD || op == SP_OP_RING_STEP)
     schedule_rows(desc, p, spk::kFwdBM, spk::kFwdBN, true, v,
                   row_fills(desc, p).size() / kItemInts);
   else if (op == SP_OP_BWD)
@@ -1022,16 +1219,18 @@ sp_status sp_attn_plan(const sp_attn_desc* desc, int32_t op, int32_t* plan) {
   Problem p;
   sp_status s = validate(desc, p);
   if (s != SP_OK) return s;
+  if (op == SP_OP_RING_STEP && !p.prefix.empty()) return SP_ERR_UNSUPPORTED;
+  const std::vector<RowTile> tiles = p.prefix.empty() ? std::vector<RowTile>() : row_tiles(desc, p);
   std::vector<int32_t> v;
   BwdPlan b{};
   if (op == SP_OP_BWD) {
-    const Costs q = schedule_rows(desc, p, spk::kDqBM, spk::kDqBN, true, v, 0);
+    const Costs q = schedule_row_items(desc, p, tiles, spk::kDqBM, spk::kDqBN, true, v, 0);
     const Costs k = schedule_keys(desc, p, spk::kDkdvBN, spk::kDkdvBQ, v, 0);
     b = plan_bwd(q, k, p.D);
   } else {
     double us;
-    b.q = choose_shape(schedule_rows(desc, p, spk::kFwdBM, spk::kFwdBN, true, v, 0), kSplitFwd, p.D,
-                       us);
+    b.q = choose_shape(schedule_row_items(desc, p, tiles, spk::kFwdBM, spk::kFwdBN, true, v, 0), kSplitFwd,
+                       p.D, us);
   }
   const int32_t r[SP_PLAN_INTS] = {b.q.split, b.q.two, b.k.split, b.k.two, b.one, b.dq_first};
   std::copy(r, r + SP_PLAN_INTS, plan);
@@ -1104,14 +1303,25 @@ static sp_status fwd_common(const sp_attn_desc* d, const void* q, const void* k,
       (o_acc && !aligned16(o_acc)) || (o_out && !aligned16(o_out)))
     return SP_ERR_INVALID_ARG;
   if (init != 0 && init != 1) return SP_ERR_INVALID_ARG;
+  const bool prefix = !p.prefix.empty();
+  if (ring && prefix) return SP_ERR_UNSUPPORTED;
   if (d->T_q == 0) return SP_OK;
   const bool include_empty = !ring || init || o_out;
   std::vector<int32_t> items;
   const std::vector<int32_t> fills = include_empty ? row_fills(d, p) : std::vector<int32_t>();
-  const Costs cost = schedule_rows(d, p, spk::kFwdBM, spk::kFwdBN, include_empty, items,
-                                   fills.size() / kItemInts);
+  const std::vector<RowTile> tiles = prefix ? row_tiles(d, p) : std::vector<RowTile>();
+  const Costs cost = schedule_row_items(d, p, tiles, spk::kFwdBM, spk::kFwdBN, include_empty, items,
+                                        fills.size() / kItemInts);
   prepend(fills, items);
   const int n_items = (int)(items.size() / kItemInts);
+  double us;
+  const spk::LaunchShape shape = choose_shape(cost, kSplitFwd, p.D, us);
+  if (prefix) {
+    const std::vector<int32_t> records =
+        place_records(d, p, tiles, shape.split, spk::fwd_tile_keys(p.D, shape.split), items, fills.size() / kItemInts,
+                      (int)items.size());
+    items.insert(items.end(), records.begin(), records.end());
+  }
   hipStream_t st = (hipStream_t)stream;
   void* items_dev = nullptr;
   if (static_ws) {
@@ -1129,7 +1339,7 @@ static sp_status fwd_common(const sp_attn_desc* d, const void* q, const void* k,
   if (n_items > 0) {
     spk::FwdArgs a{};
     spk::ItemList list{};
-    if (n_items <= spk::kInlineItems) {
+    if (items.size() <= std::size(list.v)) {
       std::copy(items.begin(), items.end(), list.v);
     } else {
       if ((s = upload(items_dev, items, st)) != SP_OK) return s;
@@ -1148,8 +1358,7 @@ static sp_status fwd_common(const sp_attn_desc* d, const void* q, const void* k,
     a.causal = d->causal;
     a.init = init;
     a.n_items = n_items;
-    double us;
-    SP_HIP(spk::launch_attn_fwd(a, list, choose_shape(cost, kSplitFwd, p.D, us), p.D, ring, st));
+    SP_HIP(spk::launch_attn_fwd(a, list, shape, p.D, ring, prefix, st));
   }
   return SP_OK;
 }
@@ -1198,29 +1407,42 @@ sp_status sp_attn_bwd(const sp_attn_desc* d, const void* q, const void* k, const
   // a dq_acc's dummy slots stay untouched
   const std::vector<int32_t> fq = dq ? row_fills(d, p) : std::vector<int32_t>();
   const std::vector<int32_t> fkv = key_fills(d, p);
+  const bool prefix = !p.prefix.empty();
+  const std::vector<RowTile> tiles = prefix ? row_tiles(d, p) : std::vector<RowTile>();
   const Costs cost_q =
-      schedule_rows(d, p, spk::kDqBM, spk::kDqBN, true, it_dq, fq.size() / kItemInts);
+      schedule_row_items(d, p, tiles, spk::kDqBM, spk::kDqBN, true, it_dq, fq.size() / kItemInts);
   prepend(fq, it_dq);
   const Costs cost_k =
       schedule_keys(d, p, spk::kDkdvBN, spk::kDkdvBQ, it_kv, fkv.size() / kItemInts);
   prepend(fkv, it_kv);
   const size_t na = it_dq.size() / kItemInts, nb = it_kv.size() / kItemInts;
-  Layout L = layout_for(d, p, SP_OP_BWD, na, nb);
+  // (the records of row tiles lie behind the dQ items, or in a launch's own list
+  // behind all items)
+  Layout L = layout_for(d, p, SP_OP_BWD, na + record_room(tiles.size()) / kItemInts, nb);
   if ((s = check_ws(L, ws, ws_bytes)) != SP_OK) return s;
   hipStream_t st = (hipStream_t)stream;
   if ((s = refuse_capture(st)) != SP_OK) return s;
   const int D = p.D;
+  const BwdPlan plan = plan_bwd(cost_q, cost_k, D);
+  const size_t n_rec = tiles.size() * plan.q.split * spk::record_ints(kSlots / plan.q.split);
+  const bool by_value = it_dq.size() + it_kv.size() + n_rec <= std::size(spk::ItemList().v);
+  const size_t rec_at = by_value ? it_dq.size() + it_kv.size() : it_dq.size();
+  std::vector<int32_t> records;
+  if (prefix)
+    records = place_records(d, p, tiles, plan.q.split, spk::kDqBN, it_dq, fq.size() / kItemInts, (int)rec_at);
   {
     // Work lists that fit a launch's arguments go there (a launch of its own
     // for dK/dV has its list first).  Else both in one copy (they are adjacent
     // in the workspace): every host-to-device copy sits between two kernels on
     // the stream.
     spk::ItemList list{};
-    const bool by_value = na + nb <= (size_t)spk::kInlineItems;
-    if (!by_value) {
+    if (by_value) {
+      std::copy(records.begin(), records.end(), list.v + rec_at);
+    } else {
       const size_t gap = (L.items_kv - L.items_dq) / sizeof(int32_t);
       std::vector<int32_t> both(gap + it_kv.size(), 0);
       std::copy(it_dq.begin(), it_dq.end(), both.begin());
+      std::copy(records.begin(), records.end(), both.begin() + rec_at);
       std::copy(it_kv.begin(), it_kv.end(), both.begin() + gap);
       if ((s = upload(at(ws, L.items_dq), both, st)) != SP_OK) return s;
     }
@@ -1250,7 +1472,6 @@ sp_status sp_attn_bwd(const sp_attn_desc* d, const void* q, const void* k, const
     b.T_q = d->T_q; b.T_k = d->T_k; b.H = d->H_loc; b.Hkv = d->Hkv_loc;
     b.scale_log2 = sl2; b.scale = d->softmax_scale; b.causal = d->causal; b.direct = p.direct;
     b.n_items = (int)nb;
-    const BwdPlan plan = plan_bwd(cost_q, cost_k, D);
     if (by_value) std::copy(it_dq.begin(), it_dq.end(), list.v);
     // dK, dV written over K, V: a key's rows are read and written by one dK/dV
     // workgroup, but dQ reads all of them, so it ends first (same splits, same
@@ -1258,9 +1479,9 @@ sp_status sp_attn_bwd(const sp_attn_desc* d, const void* q, const void* k, const
     const bool over_kv = dk == k || dk == v || dv == k || dv == v;
     if (plan.one && !over_kv) {
       if (by_value) std::copy(it_kv.begin(), it_kv.end(), list.v + it_dq.size());
-      SP_HIP(spk::launch_attn_bwd(a, b, list, plan.q, plan.k, plan.dq_first, D, st));
+      SP_HIP(spk::launch_attn_bwd(a, b, list, plan.q, plan.k, plan.dq_first, D, prefix, st));
     } else {
-      SP_HIP(spk::launch_attn_dq(a, list, plan.q, D, st));
+      SP_HIP(spk::launch_attn_dq(a, list, plan.q, D, prefix, st));
       if (by_value) std::copy(it_kv.begin(), it_kv.end(), list.v);
       SP_HIP(spk::launch_attn_dkdv(b, list, plan.k, D, st));
     }

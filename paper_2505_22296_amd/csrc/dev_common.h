@@ -3,6 +3,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "launch.h"
+
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
@@ -218,6 +220,47 @@ SP_DEV void load_item(const int32_t* items, const List& list, int base, int pos,
     for (int j = 0; j < 8; ++j) v[j] = list.v[(base + pos) * 8 + j];
   }
 }
+
+// ---- Row tiles of a batch whose segments share prefixes (SP_DESC_SHARED_PREFIX).
+// A work item names a record of int32, one for each workgroup of the item:
+//   {key tiles, first prefix key, 1 if there is a prefix, 0}
+//   1 + SL key ranges {key tiles up to its end, first key (a multiple of 8), end}:
+//     the prefix, then what the slots see of their own segments
+//   SL slots {row begin, row end, own key begin, own key end, causal delta}
+// A slot is the rows of one row group of wavefronts: up to 32 rows of one segment.
+// The workgroup's tiles walk the ranges one after the other; a wavefront skips
+// those that hold none of its own segment's keys.
+SP_DEV int32_t table_at(const int32_t* items, int i) {
+  typedef const __attribute__((address_space(4))) int32_t cint;
+  return ((cint*)items)[i];
+}
+// (from the launch's own list where `items` is null)
+template <typename List>
+SP_DEV int32_t table_at(const int32_t* items, const List& list, int i) {
+  return items ? table_at(items, i) : list.v[i];
+}
+template <typename List>
+SP_DEV spk::RowSlot load_slot(const int32_t* items, const List& list, int record, int n_slots, int slot) {
+  const int o = record + spk::kRecordRanges + 3 * (1 + n_slots) + 5 * slot;
+  return spk::RowSlot{table_at(items, list, o), table_at(items, list, o + 1), table_at(items, list, o + 2),
+                 table_at(items, list, o + 3), table_at(items, list, o + 4)};
+}
+// The range that holds key tile v; v < the record's key tiles, and does not fall
+// from call to call.
+struct KeyWalk {
+  int range = -1, v0 = 0, v1 = 0, kt0 = 0, k1 = 0;
+  template <typename List>
+  SP_DEV void seek(const int32_t* items, const List& list, int record, int v) {
+    while (v >= v1) {
+      ++range;
+      v0 = v1;
+      const int o = record + spk::kRecordRanges + 3 * range;
+      v1 = table_at(items, list, o);
+      kt0 = table_at(items, list, o + 1);
+      k1 = table_at(items, list, o + 2);
+    }
+  }
+};
 
 // Launches that split every work item over S workgroups: workgroup b runs on
 // XCD b % 8, and an XCD's S consecutive workgroups share one item of its list

@@ -64,7 +64,8 @@ struct DqStage {
 
 // `block`: the workgroup's number among the launch's dQ workgroups.  TWO: at
 // most 128 VGPRs, so that two workgroups share a CU.
-template <int D, int KW, bool TWO>
+// PFX: segments share prefixes (see the forward).
+template <int D, int KW, bool TWO, bool PFX>
 SP_DEV void dq_body(const DqArgs& a, const ItemList& list, u32x4* smem, int block) {
   using S = DqStage<D, KW>;
   constexpr int RW = S::RW, BN = S::BN, KS = D / 16, DB = D / 32, NST = S::NST, TPB = S::TPB;
@@ -75,11 +76,13 @@ SP_DEV void dq_body(const DqArgs& a, const ItemList& list, u32x4* smem, int bloc
   int32_t it[kItemInts];
   load_item(a.items, list, 0, pos, it);
   int q0 = it[0], q1 = it[1], k1 = it[3];
-  const int k0 = it[2], delta = it[4], head = it[5], kvh = it[6];
+  int k0 = it[2], delta = it[4];
+  const int head = it[5], kvh = it[6];
   const int tid = threadIdx.x;
   if constexpr (KW > 1) {
-    if (!split_rows<KW>(it[7] == kItemFillQ, 32 * RW, sub, q0, q1)) return;
-    if (a.causal) k1 = max(k0, min(k1, q1 + delta));
+    if (!PFX || it[7] == kItemFillQ)
+      if (!split_rows<KW>(it[7] == kItemFillQ, 32 * RW, sub, q0, q1)) return;
+    if (!PFX && a.causal) k1 = max(k0, min(k1, q1 + delta));
   }
   if (it[7] == kItemFillQ) {  // dummy slot of a bf16 dQ: +0
     fill_rows_bf16(a.dq, q0, q1, a.H, head, D, tid, NTQ);
@@ -88,7 +91,20 @@ SP_DEV void dq_body(const DqArgs& a, const ItemList& list, u32x4* smem, int bloc
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lane = tid & 63, hh = lane >> 5, l32 = lane & 31;
   const int rg = KW > 1 ? w % RW : w, kg = KW > 1 ? w / RW : 0;
-  const int wr0 = q0 + rg * 32;  // the wavefront's first row
+  const int record = it[0] + sub * record_ints(RW);  // PFX
+  int pk0 = 0;
+  bool has_prefix = false;
+  if constexpr (PFX) {
+    const RowSlot slot = load_slot(a.items, list, record, RW, rg);
+    q0 = slot.row0;
+    q1 = slot.row1;
+    k0 = slot.k0;
+    k1 = slot.k1;
+    delta = slot.delta;
+    pk0 = table_at(a.items, list, record + 1);
+    has_prefix = table_at(a.items, list, record + 2) != 0;
+  }
+  const int wr0 = PFX ? q0 : q0 + rg * 32;  // the wavefront's first row
   const int row = wr0 + l32;
   const bool row_ok = row < q1;
   const int lrow = row_ok ? row : q0;
@@ -121,8 +137,11 @@ SP_DEV void dq_body(const DqArgs& a, const ItemList& list, u32x4* smem, int bloc
     for (int r = 0; r < 16; ++r) acc[d][r] = 0.f;
 
   const int kt_first = k0 & ~7;
-  // stages of KW tiles
-  const int n_tiles = (k1 > k0) ? (k1 - kt_first + BN * KW - 1) / (BN * KW) : 0;
+  // stages of KW tiles (PFX: of the record's key tiles)
+  int n_keytiles = 0;
+  if constexpr (PFX) n_keytiles = table_at(a.items, list, record);
+  const int n_tiles = PFX ? (n_keytiles + KW - 1) / KW : (k1 > k0) ? (k1 - kt_first + BN * KW - 1) / (BN * KW) : 0;
+  KeyWalk walk_in, walk;  // of the copies and of the tiles in use
 
   // The wavefront's DMA blocks are rg + RW*j of the K, then the V blocks; a
   // block holds 16 rows of one 32-dim sub-tile, block b rows 16 (b % 2) .. of
@@ -135,8 +154,16 @@ SP_DEV void dq_body(const DqArgs& a, const ItemList& list, u32x4* smem, int bloc
   const int off = 2 * (key_of * kstride + blk_chunk(key_of, lane & 3) * 8);  // bytes
   const uint16_t* kbase = a.k + (int64_t)kvh * D;
   const uint16_t* vbase = a.v + (int64_t)kvh * D;
+  const int kend = k1;
   auto issue = [&](int n) {
-    const int kt = kt_first + (n * KW + kg) * BN;
+    int kt = kt_first + (n * KW + kg) * BN, k1 = kend;
+    if constexpr (PFX) {
+      const int v = n * KW + kg;
+      if (KW > 1 && v >= n_keytiles) return;
+      walk_in.seek(a.items, list, record, v);
+      kt = walk_in.kt0 + (v - walk_in.v0) * BN;
+      k1 = walk_in.k1;
+    }
     if (KW > 1 && kt >= k1) return;  // the key group has no tile in the last stage
     u32x4* stg = smem + (n % NST) * STAGE + kg * S::TILE;
     const int64_t rowoff = (int64_t)kt * kstride;
@@ -170,8 +197,18 @@ SP_DEV void dq_body(const DqArgs& a, const ItemList& list, u32x4* smem, int bloc
         for (int t = 0; t < TPB; ++t)
           if (n + NST - TPB + t < n_tiles) issue(n + NST - TPB + t);
       }
-      const int kt = kt_first + (n * KW + kg) * BN;
-      if (kt >= wave_kmax) continue;  // wholly past this wavefront's rows
+      int kt = kt_first + (n * KW + kg) * BN;
+      bool in_prefix = false;
+      if constexpr (PFX) {
+        const int v = n * KW + kg;
+        if (KW > 1 && v >= n_keytiles) continue;
+        walk.seek(a.items, list, record, v);
+        kt = walk.kt0 + (v - walk.v0) * BN;
+        in_prefix = has_prefix && walk.range == 0;
+        if (in_prefix ? wave_rows <= 0 : (kt >= wave_kmax) | (kt + BN <= k0)) continue;
+      } else {
+        if (kt >= wave_kmax) continue;  // wholly past this wavefront's rows
+      }
       const u32x4* stg = smem + u * STAGE + kg * S::TILE;
 
       // K and V fragments of the tile, all read before the first MFMA (TWO:
@@ -233,11 +270,14 @@ SP_DEV void dq_body(const DqArgs& a, const ItemList& list, u32x4* smem, int bloc
         read_kt();
         __builtin_amdgcn_sched_barrier(0);
       }
-      const bool need_mask = (kt < k0) | (kt + BN > k1) | (a.causal & (kt + BN - 1 > wr0 + delta));
+      // (the whole prefix is visible to every row)
+      const int m0 = PFX && in_prefix ? pk0 : k0, m1 = PFX && in_prefix ? walk.k1 : k1;
+      const int causal = PFX && in_prefix ? 0 : a.causal;
+      const bool need_mask = (kt < m0) | (kt + BN > m1) | (causal & (kt + BN - 1 > wr0 + delta));
       if (need_mask) {
         // keys [lo, hi) of the lane half's, counted from kt + 8 hh
-        const int lo = k0 - kt - hh * 8;
-        const int hi = (a.causal ? min(k1, row + delta + 1) : k1) - kt - hh * 8;
+        const int lo = m0 - kt - hh * 8;
+        const int hi = (causal ? min(m1, row + delta + 1) : m1) - kt - hh * 8;
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
           const int key = c_row_of(r, 0);
@@ -323,10 +363,10 @@ SP_DEV void dq_body(const DqArgs& a, const ItemList& list, u32x4* smem, int bloc
   }
 }
 
-template <int D, int KW, bool TWO>
+template <int D, int KW, bool TWO, bool PFX>
 __global__ __launch_bounds__(NTQ, TWO ? 4 : 1) void attn_dq_kernel(DqArgs a, ItemList list) {
   __shared__ u32x4 smem[DqStage<D, KW>::SMEM];
-  dq_body<D, KW, TWO>(a, list, smem, blockIdx.x);
+  dq_body<D, KW, TWO, PFX>(a, list, smem, blockIdx.x);
 }
 
 // ---------------------------------------------------------------- dK / dV
@@ -655,7 +695,7 @@ __global__ __launch_bounds__(64 * 2 * NPF, TWO ? 4 : 1) void attn_dkdv_kernel(Dk
 // mask 245 / 193).  Workgroups
 // [0, n_first) run the list with the longer workgroups: 28 heads of 2048 rows
 // 148 us with dQ, whose items are the longer ones there, first, 160 us last.
-template <int D, int KW, int RG, bool TWO>
+template <int D, int KW, int RG, bool TWO, bool PFX>
 __global__ __launch_bounds__(NTQ, TWO ? 4 : 1) void attn_bwd_kernel(DqArgs a, DkdvArgs b, ItemList list,
                                                           int n_first, int dq_first) {
   static_assert(NTQ == 64 * 2 * NPF, "one workgroup size");
@@ -665,7 +705,7 @@ __global__ __launch_bounds__(NTQ, TWO ? 4 : 1) void attn_bwd_kernel(DqArgs a, Dk
   const bool first = (int)blockIdx.x < n_first;
   const int block = first ? blockIdx.x : blockIdx.x - n_first;
   if (first == (dq_first != 0))
-    dq_body<D, KW, TWO>(a, list, smem, block);
+    dq_body<D, KW, TWO, PFX>(a, list, smem, block);
   else
     dkdv_wg<D, RG, TWO>(b, list, a.n_items, smem, block);
 }
@@ -673,23 +713,23 @@ __global__ __launch_bounds__(NTQ, TWO ? 4 : 1) void attn_bwd_kernel(DqArgs a, Dk
 }  // namespace
 
 template <int D, int KW, bool TWO>
-static hipError_t launch_dq(const DqArgs& a, const ItemList& list, hipStream_t st) {
-  return sp_launch(kKDq, attn_dq_kernel<D, KW, TWO>, dim3(split_grid(a.n_items, KW)), dim3(NTQ), st,
-                   a, list);
+static hipError_t launch_dq(const DqArgs& a, const ItemList& list, bool prefix, hipStream_t st) {
+  return sp_launch(kKDq, prefix ? attn_dq_kernel<D, KW, TWO, true> : attn_dq_kernel<D, KW, TWO, false>,
+                   dim3(split_grid(a.n_items, KW)), dim3(NTQ), st, a, list);
 }
 
-hipError_t launch_attn_dq(const DqArgs& a, const ItemList& list, LaunchShape s, int D,
+hipError_t launch_attn_dq(const DqArgs& a, const ItemList& list, LaunchShape s, int D, bool prefix,
                           hipStream_t st) {
   if (a.n_items <= 0) return hipSuccess;
   if (D == 128) {
-    if (s.split == 4) return launch_dq<128, 4, false>(a, list, st);
-    if (s.split == 2) return launch_dq<128, 2, false>(a, list, st);
-    return launch_dq<128, 1, false>(a, list, st);
+    if (s.split == 4) return launch_dq<128, 4, false>(a, list, prefix, st);
+    if (s.split == 2) return launch_dq<128, 2, false>(a, list, prefix, st);
+    return launch_dq<128, 1, false>(a, list, prefix, st);
   }
-  if (s.split == 4) return launch_dq<64, 4, false>(a, list, st);
-  if (s.split == 2) return launch_dq<64, 2, false>(a, list, st);
-  if (s.two) return launch_dq<64, 1, true>(a, list, st);
-  return launch_dq<64, 1, false>(a, list, st);
+  if (s.split == 4) return launch_dq<64, 4, false>(a, list, prefix, st);
+  if (s.split == 2) return launch_dq<64, 2, false>(a, list, prefix, st);
+  if (s.two) return launch_dq<64, 1, true>(a, list, prefix, st);
+  return launch_dq<64, 1, false>(a, list, prefix, st);
 }
 
 template <int D, int RG, bool TWO>
@@ -711,32 +751,32 @@ hipError_t launch_attn_dkdv(const DkdvArgs& a, const ItemList& list, LaunchShape
 
 template <int D, int KW, int RG, bool TWO>
 static hipError_t launch_bwd(const DqArgs& a, const DkdvArgs& b, const ItemList& list,
-                             bool dq_first, hipStream_t st) {
+                             bool dq_first, bool prefix, hipStream_t st) {
   // the first list's workgroups are rounded up to eight, so that the second
   // list's positions keep their XCDs
   const int nq = split_grid(a.n_items, KW), nk = split_grid(b.n_items, RG);
   const int n_first = ((dq_first ? nq : nk) + 7) / 8 * 8;
   const dim3 grid(n_first + (dq_first ? nk : nq)), block(NTQ);
-  return sp_launch2(kKDq, kKDkdv, attn_bwd_kernel<D, KW, RG, TWO>, grid, block, st, a, b, list,
-                    n_first, (int)dq_first);
+  return sp_launch2(kKDq, kKDkdv, prefix ? attn_bwd_kernel<D, KW, RG, TWO, true> : attn_bwd_kernel<D, KW, RG, TWO, false>,
+                    grid, block, st, a, b, list, n_first, (int)dq_first);
 }
 
 hipError_t launch_attn_bwd(const DqArgs& a, const DkdvArgs& b, const ItemList& list, LaunchShape q,
-                           LaunchShape k, bool dq_first, int D, hipStream_t st) {
+                           LaunchShape k, bool dq_first, int D, bool prefix, hipStream_t st) {
   if (D == 128) {
     if (q.split == 4 && k.split == 2)
-      return launch_bwd<128, 4, 2, false>(a, b, list, dq_first, st);
+      return launch_bwd<128, 4, 2, false>(a, b, list, dq_first, prefix, st);
     if (q.split == 2 && k.split == 1)
-      return launch_bwd<128, 2, 1, false>(a, b, list, dq_first, st);
+      return launch_bwd<128, 2, 1, false>(a, b, list, dq_first, prefix, st);
     if (q.split == 1 && k.split == 1)
-      return launch_bwd<128, 1, 1, false>(a, b, list, dq_first, st);
+      return launch_bwd<128, 1, 1, false>(a, b, list, dq_first, prefix, st);
     return hipErrorInvalidValue;
   }
-  if (q.split == 4 && k.split == 2) return launch_bwd<64, 4, 2, false>(a, b, list, dq_first, st);
-  if (q.split == 2 && k.split == 1) return launch_bwd<64, 2, 1, false>(a, b, list, dq_first, st);
+  if (q.split == 4 && k.split == 2) return launch_bwd<64, 4, 2, false>(a, b, list, dq_first, prefix, st);
+  if (q.split == 2 && k.split == 1) return launch_bwd<64, 2, 1, false>(a, b, list, dq_first, prefix, st);
   if (q.split == 1 && k.split == 1)
-    return q.two ? launch_bwd<64, 1, 1, true>(a, b, list, dq_first, st)
-                 : launch_bwd<64, 1, 1, false>(a, b, list, dq_first, st);
+    return q.two ? launch_bwd<64, 1, 1, true>(a, b, list, dq_first, prefix, st)
+                 : launch_bwd<64, 1, 1, false>(a, b, list, dq_first, prefix, st);
   return hipErrorInvalidValue;
 }
 

@@ -53,9 +53,7 @@ static_assert(kFwdBM == 32 * NW, "fwd tiling");
 template <int D, int KW>
 struct FwdStage {
   static constexpr int RW = NW / KW;           // row groups of 32 rows
-  // keys per tile: 32 where KW tiles of 64 keys would leave no room for the
-  // next ones beside them
-  static constexpr int BN = KW * D > 256 ? 32 : kFwdBN;
+  static constexpr int BN = fwd_tile_keys(D, KW);  // keys per tile
   static constexpr int NST = KW == 1 ? kFwdStages : 2;         // resident stages
   static constexpr int TPB = KW == 1 ? kFwdTilesPerSync : 1;   // stages per barrier
   static_assert(NST % TPB == 0 && NST >= 2 * TPB, "fwd pipeline");
@@ -77,7 +75,9 @@ struct FwdStage {
 // over KW workgroups (of 256 / KW rows each), all on the item's XCD, one
 // after the other, the last rows (the longest under a causal mask) first.
 // TWO: at most 128 VGPRs, so that two workgroups share a CU.
-template <int D, bool MERGE, int KW, bool TWO>
+// PFX: segments share prefixes; the items name records of slots and key ranges
+// (dev_common.h), the workgroup's rows come from several segments.
+template <int D, bool MERGE, int KW, bool TWO, bool PFX>
 __global__ __launch_bounds__(NT, TWO ? 4 : 1) void attn_fwd_kernel(FwdArgs a, ItemList list) {
   using S = FwdStage<D, KW>;
   constexpr int RW = S::RW, BN = S::BN, NST = S::NST, TPB = S::TPB;
@@ -92,12 +92,15 @@ __global__ __launch_bounds__(NT, TWO ? 4 : 1) void attn_fwd_kernel(FwdArgs a, It
   if (!split_pos<KW>(blockIdx.x, a.n_items, pos, sub)) return;
   int32_t it[kItemInts];
   load_item(a.items, list, 0, pos, it);
+  static_assert(!PFX || !MERGE, "a ring step has no shared prefixes");
   int q0 = it[0], q1 = it[1], k1 = it[3];
-  const int k0 = it[2], delta = it[4], head = it[5], kvh = it[6];
+  int k0 = it[2], delta = it[4];
+  const int head = it[5], kvh = it[6];
   const int tid = threadIdx.x;
   if constexpr (KW > 1) {
-    if (!split_rows<KW>(it[7] == kItemFillQ, 32 * RW, sub, q0, q1)) return;
-    if (a.causal) k1 = max(k0, min(k1, q1 + delta));
+    if (!PFX || it[7] == kItemFillQ)
+      if (!split_rows<KW>(it[7] == kItemFillQ, 32 * RW, sub, q0, q1)) return;
+    if (!PFX && a.causal) k1 = max(k0, min(k1, q1 + delta));
   }
   if (it[7] == kItemFillQ) {
     // dummy slot: O = +0, LSE = -inf (ring: the accumulators' identity on the
@@ -117,10 +120,24 @@ __global__ __launch_bounds__(NT, TWO ? 4 : 1) void attn_fwd_kernel(FwdArgs a, It
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lane = tid & 63, hh = lane >> 5, l32 = lane & 31;
   const int rg = KW > 1 ? w % RW : w, kg = KW > 1 ? w / RW : 0;
-  const int wr0 = q0 + rg * 32;  // the wavefront's first row
+  const int record = it[0] + sub * record_ints(RW);  // PFX
+  int pk0 = 0;
+  bool has_prefix = false;
+  if constexpr (PFX) {
+    const RowSlot slot = load_slot(a.items, list, record, RW, rg);
+    q0 = slot.row0;
+    q1 = slot.row1;
+    k0 = slot.k0;
+    k1 = slot.k1;
+    delta = slot.delta;
+    pk0 = table_at(a.items, list, record + 1);
+    has_prefix = table_at(a.items, list, record + 2) != 0;
+  }
+  const int wr0 = PFX ? q0 : q0 + rg * 32;  // the wavefront's first row
   const int row = wr0 + l32;
   const bool row_ok = row < q1;
-  // last key any row of this wavefront may see (tiles past it are skipped)
+  // last key any row of this wavefront may see (tiles past it are skipped; PFX:
+  // of its own segment)
   const int wave_rows = min(32, q1 - wr0);
   const int wave_kmax = wave_rows <= 0 ? -1 : a.causal ? min(k1, wr0 + wave_rows + delta) : k1;
 
@@ -149,8 +166,11 @@ __global__ __launch_bounds__(NT, TWO ? 4 : 1) void attn_fwd_kernel(FwdArgs a, It
   float msc = 0.f, m_thr = neg_inf();
 
   const int kt_first = k0 & ~7;
-  // stages of KW tiles
-  const int n_tiles = (k1 > k0) ? (k1 - kt_first + BN * KW - 1) / (BN * KW) : 0;
+  // stages of KW tiles (PFX: of the record's key tiles)
+  int n_keytiles = 0;
+  if constexpr (PFX) n_keytiles = table_at(a.items, list, record);
+  const int n_tiles = PFX ? (n_keytiles + KW - 1) / KW : (k1 > k0) ? (k1 - kt_first + BN * KW - 1) / (BN * KW) : 0;
+  KeyWalk walk_in, walk;  // of the copies and of the tiles in use
 
   // Per-lane, tile-independent element offsets of this wavefront's DMA
   // blocks rg + RW*j: the first NBK of them in the K tile, the rest in V;
@@ -166,8 +186,16 @@ __global__ __launch_bounds__(NT, TWO ? 4 : 1) void attn_fwd_kernel(FwdArgs a, It
   }
   const uint16_t* kbase = a.k + (int64_t)kvh * D;
   const uint16_t* vbase = a.v + (int64_t)kvh * D;
+  const int kend = k1;
   auto issue = [&](int n) {
-    const int kt = kt_first + (n * KW + kg) * BN;
+    int kt = kt_first + (n * KW + kg) * BN, k1 = kend;
+    if constexpr (PFX) {
+      const int v = n * KW + kg;
+      if (KW > 1 && v >= n_keytiles) return;
+      walk_in.seek(a.items, list, record, v);
+      kt = walk_in.kt0 + (v - walk_in.v0) * BN;
+      k1 = walk_in.k1;
+    }
     if (KW > 1 && kt >= k1) return;  // the key group has no tile in the last stage
     u32x4* stg = smem + (n % NST) * STAGE + kg * S::TILE + rg * 64;
     const int64_t rowoff = (int64_t)kt * kstride;
@@ -215,8 +243,21 @@ __global__ __launch_bounds__(NT, TWO ? 4 : 1) void attn_fwd_kernel(FwdArgs a, It
       // stage n + NST - TPB was freed at the last barrier; its copy is issued
       // after this tile's first MFMAs (spreads the DMA burst)
       const bool pf = KW < 4 && n + NST - TPB < n_tiles;
-      const int kt = kt_first + (n * KW + kg) * BN;
-      if (kt >= wave_kmax) {  // wholly past this wavefront's rows
+      int kt = kt_first + (n * KW + kg) * BN;
+      bool in_prefix = false, skip;
+      if constexpr (PFX) {
+        const int v = n * KW + kg;
+        skip = KW > 1 && v >= n_keytiles;
+        if (!skip) {
+          walk.seek(a.items, list, record, v);
+          kt = walk.kt0 + (v - walk.v0) * BN;
+          in_prefix = has_prefix && walk.range == 0;
+          skip = in_prefix ? wave_rows <= 0 : (kt >= wave_kmax) | (kt + BN <= k0);
+        }
+      } else {
+        skip = kt >= wave_kmax;  // wholly past this wavefront's rows
+      }
+      if (skip) {
         if (pf) issue(n + NST - TPB);
         continue;
       }
@@ -262,11 +303,14 @@ __global__ __launch_bounds__(NT, TWO ? 4 : 1) void attn_fwd_kernel(FwdArgs a, It
       if (pf) issue(n + NST - TPB);
 
       // ---- mask (only on edge / diagonal tiles)
-      const bool need_mask = (kt < k0) | (kt + BN > k1) | (a.causal & (kt + BN - 1 > wr0 + delta));
+      // (the whole prefix is visible to every row)
+      const int m0 = PFX && in_prefix ? pk0 : k0, m1 = PFX && in_prefix ? walk.k1 : k1;
+      const int causal = PFX && in_prefix ? 0 : a.causal;
+      const bool need_mask = (kt < m0) | (kt + BN > m1) | (causal & (kt + BN - 1 > wr0 + delta));
       if (need_mask) {
         // keys [lo, hi) of the lane half's, counted from kt + 8 hh
-        const int lo = k0 - kt - hh * 8;
-        const int hi = (a.causal ? min(k1, row + delta + 1) : k1) - kt - hh * 8;
+        const int lo = m0 - kt - hh * 8;
+        const int hi = (causal ? min(m1, row + delta + 1) : m1) - kt - hh * 8;
 #pragma unroll
         for (int g = 0; g < G; ++g)
 #pragma unroll
@@ -434,26 +478,28 @@ __global__ __launch_bounds__(NT, TWO ? 4 : 1) void attn_fwd_kernel(FwdArgs a, It
 }  // namespace
 
 template <int D, int KW, bool TWO>
-static hipError_t launch_fwd(const FwdArgs& a, const ItemList& list, bool merge, hipStream_t st) {
+static hipError_t launch_fwd(const FwdArgs& a, const ItemList& list, bool merge, bool prefix, hipStream_t st) {
   const dim3 grid(split_grid(a.n_items, KW)), block(NT);
-  return merge ? sp_launch(kKFwd, attn_fwd_kernel<D, true, KW, TWO>, grid, block, st, a, list)
-               : sp_launch(kKFwd, attn_fwd_kernel<D, false, KW, TWO>, grid, block, st, a, list);
+  return merge    ? sp_launch(kKFwd, attn_fwd_kernel<D, true, KW, TWO, false>, grid, block, st, a, list)
+         : prefix ? sp_launch(kKFwd, attn_fwd_kernel<D, false, KW, TWO, true>, grid, block, st, a, list)
+                  : sp_launch(kKFwd, attn_fwd_kernel<D, false, KW, TWO, false>, grid, block, st, a, list);
 }
 
-hipError_t launch_attn_fwd(const FwdArgs& a, const ItemList& list, LaunchShape s, int D, bool merge,
+hipError_t launch_attn_fwd(const FwdArgs& a, const ItemList& list, LaunchShape s, int D, bool merge, bool prefix,
                            hipStream_t st) {
   if (a.n_items <= 0) return hipSuccess;
+  if (merge && prefix) return hipErrorInvalidValue;
   if (D == 128) {
-    if (s.split == 4) return launch_fwd<128, 4, false>(a, list, merge, st);
-    if (s.split == 2) return launch_fwd<128, 2, false>(a, list, merge, st);
-    return launch_fwd<128, 1, false>(a, list, merge, st);
+    if (s.split == 4) return launch_fwd<128, 4, false>(a, list, merge, prefix, st);
+    if (s.split == 2) return launch_fwd<128, 2, false>(a, list, merge, prefix, st);
+    return launch_fwd<128, 1, false>(a, list, merge, prefix, st);
   }
-  if (s.split == 4) return launch_fwd<64, 4, false>(a, list, merge, st);
+  if (s.split == 4) return launch_fwd<64, 4, false>(a, list, merge, prefix, st);
   if (s.split == 2)
-    return s.two ? launch_fwd<64, 2, true>(a, list, merge, st)
-                 : launch_fwd<64, 2, false>(a, list, merge, st);
-  if (s.two) return launch_fwd<64, 1, true>(a, list, merge, st);
-  return launch_fwd<64, 1, false>(a, list, merge, st);
+    return s.two ? launch_fwd<64, 2, true>(a, list, merge, prefix, st)
+                 : launch_fwd<64, 2, false>(a, list, merge, prefix, st);
+  if (s.two) return launch_fwd<64, 1, true>(a, list, merge, prefix, st);
+  return launch_fwd<64, 1, false>(a, list, merge, prefix, st);
 }
 
 }  // namespace spk

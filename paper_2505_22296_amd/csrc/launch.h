@@ -129,6 +129,9 @@ struct ReduceArgs {
 // Work item of the attention kernels: 8 int32.
 //   fwd / dq:  {q_begin, q_end, k_begin, k_end, delta, head, kv_head, 0}
 //   dk/dv:     {k_begin, k_end, q_begin, q_end, delta, head, kv_head, 1}
+//   fwd / dq of a batch with shared prefixes:
+//              {record, 0, 0, 0, 0, head, kv_head, 0}: the record of the item's
+//              first workgroup, in ints from the list's start (layout: RowSlot)
 //   zero fill of a dummy query slot (fwd / dq): {r_begin, r_end, 0, 0, 0, slot, 0, 2}
 //   zero fill of a KV head no real query head reads (dk/dv):
 //              {k_begin, k_end, 0, 0, 0, 0, kv_head, 3}
@@ -246,13 +249,15 @@ struct LaunchShape {
   int split;
   bool two;
 };
-hipError_t launch_attn_fwd(const FwdArgs& a, const ItemList& list, LaunchShape s, int D, bool merge, hipStream_t st);
-hipError_t launch_attn_dq(const DqArgs& a, const ItemList& list, LaunchShape s, int D, hipStream_t st);
+// `prefix`: the row items name records (shared prefixes); not with `merge`.
+hipError_t launch_attn_fwd(const FwdArgs& a, const ItemList& list, LaunchShape s, int D, bool merge, bool prefix,
+                           hipStream_t st);
+hipError_t launch_attn_dq(const DqArgs& a, const ItemList& list, LaunchShape s, int D, bool prefix, hipStream_t st);
 hipError_t launch_attn_dkdv(const DkdvArgs& a, const ItemList& list, LaunchShape s, int D, hipStream_t st);
 // dQ and dK/dV in one launch; (q.split, k.split) one of (4, 2), (2, 1),
 // (1, 1); two workgroups a CU for (1, 1) alone, q.two.  `dq_first`: the dQ workgroups come first.
 hipError_t launch_attn_bwd(const DqArgs& a, const DkdvArgs& b, const ItemList& list, LaunchShape q,
-                           LaunchShape k, bool dq_first, int D, hipStream_t st);
+                           LaunchShape k, bool dq_first, int D, bool prefix, hipStream_t st);
 
 // Tile sizes the host scheduler must use (rows per fwd/dq item, keys per
 // dk/dv item) and the kernels' LDS pipelines.
@@ -266,6 +271,18 @@ static constexpr int kDqBM = 32 * kDqWaves;
 static constexpr int kDqBN = 32;
 static constexpr int kDqStages = 4;
 static constexpr int kDqTilesPerSync = 2;
+// keys per tile of a forward split over `split` workgroups: 32 where that many
+// tiles of 64 keys would leave no room for the next ones beside them
+static constexpr int fwd_tile_keys(int D, int split) { return split * D > 256 ? 32 : kFwdBN; }
+// Rows of one segment in a row tile with shared prefixes: rows [row0, row1) see keys
+// [k0, k1) of their own segment, under a causal mask those j <= row + delta.
+struct RowSlot {
+  int row0, row1, k0, k1, delta;
+};
+// Ints before the key ranges of a workgroup's record (RowSlot in dev_common.h).
+static constexpr int kRecordRanges = 4;
+// Ints of a workgroup's record with n slots, rounded up to whole items.
+static constexpr int record_ints(int n_slots) { return 8 * (n_slots + 1); }
 static constexpr int kDkdvWaves = 8;                // wavefronts per dK/dV workgroup (4 pairs)
 static constexpr int kDkdvBN = 16 * kDkdvWaves;     // keys per dK/dV item
 static constexpr int kDkdvBQ = 32;                  // query rows per chunk
