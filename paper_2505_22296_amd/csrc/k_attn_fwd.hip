@@ -244,20 +244,33 @@ __global__ __launch_bounds__(NT, TWO ? 4 : 1) void attn_fwd_kernel(FwdArgs a, It
       // after this tile's first MFMAs (spreads the DMA burst)
       const bool pf = KW < 4 && n + NST - TPB < n_tiles;
       int kt = kt_first + (n * KW + kg) * BN;
-      bool in_prefix = false, skip;
+      // what the wavefront sees of the tile: keys [m0, m1), under the causal rule if
+      // `causal`, none of them where kt >= kmax
+      int m0 = k0, m1 = k1, causal = a.causal, kmax = wave_kmax;
       if constexpr (PFX) {
         const int v = n * KW + kg;
-        skip = KW > 1 && v >= n_keytiles;
-        if (!skip) {
-          walk.seek(a.items, list, record, v);
-          kt = walk.kt0 + (v - walk.v0) * BN;
-          in_prefix = has_prefix && walk.range == 0;
-          skip = in_prefix ? wave_rows <= 0 : (kt >= wave_kmax) | (kt + BN <= k0);
+        bool live = KW == 1 || v < n_keytiles;
+        if (live) walk.seek(a.items, list, record, v);
+        kt = walk.kt0 + (v - walk.v0) * BN;
+        const bool in_prefix = has_prefix & (walk.range == 0);  // visible to every row
+        if (in_prefix) {
+          m0 = pk0;
+          m1 = walk.k1;
+          causal = 0;
+          kmax = wave_rows > 0 ? m1 : -1;
         }
-      } else {
-        skip = kt >= wave_kmax;  // wholly past this wavefront's rows
+        live &= kt + BN > m0;
+        // The values are made opaque: the compiler otherwise keeps a path for tiles
+        // of the prefix beside the one for own keys, moves the accumulators from one
+        // to the other and spills (D = 128: 34 registers; 64 answers of 256 rows to
+        // 16384 keys, 4 heads, 702 instead of 502 us)
+        m0 = __builtin_amdgcn_readfirstlane(m0);
+        m1 = __builtin_amdgcn_readfirstlane(m1);
+        causal = __builtin_amdgcn_readfirstlane(causal);
+        kmax = __builtin_amdgcn_readfirstlane(live ? kmax : 0);
+        kt = __builtin_amdgcn_readfirstlane(kt);
       }
-      if (skip) {
+      if (kt >= kmax) {  // nothing of it for this wavefront's rows
         if (pf) issue(n + NST - TPB);
         continue;
       }
@@ -303,9 +316,6 @@ __global__ __launch_bounds__(NT, TWO ? 4 : 1) void attn_fwd_kernel(FwdArgs a, It
       if (pf) issue(n + NST - TPB);
 
       // ---- mask (only on edge / diagonal tiles)
-      // (the whole prefix is visible to every row)
-      const int m0 = PFX && in_prefix ? pk0 : k0, m1 = PFX && in_prefix ? walk.k1 : k1;
-      const int causal = PFX && in_prefix ? 0 : a.causal;
       const bool need_mask = (kt < m0) | (kt + BN > m1) | (causal & (kt + BN - 1 > wr0 + delta));
       if (need_mask) {
         // keys [lo, hi) of the lane half's, counted from kt + 8 hh
