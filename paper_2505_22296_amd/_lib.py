@@ -366,19 +366,18 @@ def _device_of(stream) -> int:
     return torch.cuda.current_device() if stream is None else stream.device.index
 
 
-def _arg(t, name: str, dtype, shape, device: int, optional: bool = False, rows: bool = False):
-    """Device pointer of a tensor argument.  The library reads memory by the
-    sizes it is told, so type, shape, device and layout are checked here
-    (`rows`: tokens may lie further apart than their heads need)."""
+def _arg(t, name: str, dtype, shape: tuple, device: int, optional: bool = False):
+    """Device pointer of a contiguous tensor argument.  The library reads memory
+    by the sizes it is told, so type, shape, device and layout are checked here."""
     if t is None and optional:
         return None
-    if t is None or t.dtype != dtype or tuple(t.shape) != shape:
+    if t is None or t.dtype is not dtype or t.shape != shape:
         raise ValueError(f"{name} must be a {dtype} tensor of shape {list(shape)}, got "
                          + ("none" if t is None else f"{t.dtype} {list(t.shape)}"))
-    if not t.is_cuda or t.device.index != device:
+    if t.get_device() != device:
         raise ValueError(f"{name} must be on GPU {device}, where its stream is: it is on {t.device}")
-    if not (t[0].is_contiguous() if rows and shape[0] > 0 else t.is_contiguous()):
-        raise ValueError(f"{name} must be contiguous" + (" within a token" if rows else ""))
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
     return t.data_ptr()
 
 
@@ -403,15 +402,23 @@ def sp_policy_workspace_size(T: int, V: int) -> int:
     return n.value
 
 
-def _workspace(need: int, workspace, dev: int):
+def _outs(given, dtype, device, dev):
+    """Outputs and their pointers: each (tensor or None, name, shape), allocated
+    here where it is None (one that is given is checked)."""
+    import torch
+    ts = [torch.empty(s, dtype=dtype, device=device) if t is None else t for t, _, s in given]
+    return ts, [t.data_ptr() if g is None else _arg(g, n, dtype, s, dev) for t, (g, n, s) in zip(ts, given)]
+
+
+def _workspace(need: int, workspace, device, dev: int):
     """The caller's workspace, or one allocated here if there is none or it is
     too small."""
     import torch
-    if workspace is not None and workspace.numel() * workspace.element_size() >= need:
-        if not workspace.is_cuda or workspace.device.index != dev or not workspace.is_contiguous():
-            raise ValueError(f"workspace must be contiguous on GPU {dev}")
-        return workspace
-    return torch.empty(need, dtype=torch.uint8, device=f"cuda:{dev}")
+    if workspace is None or workspace.numel() * workspace.element_size() < need:
+        return torch.empty(need, dtype=torch.uint8, device=device)
+    if workspace.get_device() != dev or not workspace.is_contiguous():
+        raise ValueError(f"workspace must be contiguous on GPU {dev}")
+    return workspace
 
 
 def sp_policy_loss(params: PolicyParams, logits, labels, old_logp, ref_logp, advantages, cu_seqlens,
@@ -428,21 +435,18 @@ def sp_policy_loss(params: PolicyParams, logits, labels, old_logp, ref_logp, adv
     f, dev = torch.float32, _device_of(stream)
     per = T if params.c.adv_per_token else n
     args = (_arg(logits, "logits", torch.bfloat16, (T, V), dev), _arg(labels, "labels", torch.int32, (T,), dev),
-            _arg(old_logp, "old_logp", f, (T,), dev), _arg(ref_logp, "ref_logp", f, (T,), dev, optional=True),
+            _arg(old_logp, "old_logp", f, (T,), dev), _arg(ref_logp, "ref_logp", f, (T,), dev, True),
             _arg(advantages, "advantages", f, (per,), dev))
+    given = [(logp, "logp", (T,)), (lse, "lse", (T,)), (seq_sum, "seq_sum", (n,)), (seq_stats, "seq_stats", (n, 4))]
+    if with_entropy:
+        given.append((entropy, "entropy", (T,)))
     with _alloc_on(stream):
-        def out(t, *shape):
-            return torch.empty(shape, dtype=f, device=logits.device) if t is None else t
-        logp, lse, seq_sum, seq_stats = out(logp, T), out(lse, T), out(seq_sum, n), out(seq_stats, n, 4)
-        if with_entropy:
-            entropy = out(entropy, T)
-        outs = (_arg(logp, "logp", f, (T,), dev), _arg(lse, "lse", f, (T,), dev),
-                _arg(entropy, "entropy", f, (T,), dev, optional=True), _arg(seq_sum, "seq_sum", f, (n,), dev),
-                _arg(seq_stats, "seq_stats", f, (n, 4), dev))
-        ws = _workspace(sp_policy_workspace_size(T, V), workspace, dev)
-        _check(load().sp_policy_loss(params.ref, *args, T, V, cup, n, *outs, ws.data_ptr(),
-                                     ws.numel() * ws.element_size(), _stream(stream)), "sp_policy_loss")
-    return logp, lse, entropy, seq_sum, seq_stats
+        ts, ps = _outs(given, f, logits.device, dev)
+        ws = _workspace(sp_policy_workspace_size(T, V), workspace, logits.device, dev)
+        _check(load().sp_policy_loss(params.ref, *args, T, V, cup, n, ps[0], ps[1], ps[4] if with_entropy else None,
+                                     ps[2], ps[3], ws.data_ptr(), ws.numel() * ws.element_size(), _stream(stream)),
+               "sp_policy_loss")
+    return ts[0], ts[1], ts[4] if with_entropy else None, ts[2], ts[3]
 
 
 def sp_policy_loss_bwd(params: PolicyParams, logits, labels, logp, lse, entropy, old_logp, ref_logp, advantages,
@@ -453,20 +457,18 @@ def sp_policy_loss_bwd(params: PolicyParams, logits, labels, logp, lse, entropy,
     T, V = logits.shape
     cu, cup, n = _cu(cu_seqlens)
     n = max(n, 0)
-    f, dev = torch.float32, _device_of(stream)
+    f, bf, dev = torch.float32, torch.bfloat16, _device_of(stream)
     per = T if params.c.adv_per_token else n
-    args = (_arg(logits, "logits", torch.bfloat16, (T, V), dev), _arg(labels, "labels", torch.int32, (T,), dev),
-            _arg(logp, "logp", f, (T,), dev), _arg(lse, "lse", f, (T,), dev),
-            _arg(entropy, "entropy", f, (T,), dev, optional=True), _arg(old_logp, "old_logp", f, (T,), dev),
-            _arg(ref_logp, "ref_logp", f, (T,), dev, optional=True), _arg(advantages, "advantages", f, (per,), dev))
+    args = (_arg(logits, "logits", bf, (T, V), dev), _arg(labels, "labels", torch.int32, (T,), dev),
+            _arg(logp, "logp", f, (T,), dev), _arg(lse, "lse", f, (T,), dev), _arg(entropy, "entropy", f, (T,), dev, True),
+            _arg(old_logp, "old_logp", f, (T,), dev), _arg(ref_logp, "ref_logp", f, (T,), dev, True),
+            _arg(advantages, "advantages", f, (per,), dev))
     grad = _arg(grad_seq, "grad_seq", f, (n,), dev)
     with _alloc_on(stream):
-        if dlogits is None:
-            dlogits = torch.empty_like(logits)
-        _check(load().sp_policy_loss_bwd(params.ref, *args, T, V, cup, n, grad,
-                                         _arg(dlogits, "dlogits", torch.bfloat16, (T, V), dev), _stream(stream)),
+        (out,), (p,) = _outs([(dlogits, "dlogits", (T, V))], bf, logits.device, dev)
+        _check(load().sp_policy_loss_bwd(params.ref, *args, T, V, cup, n, grad, p, _stream(stream)),
                "sp_policy_loss_bwd")
-    return dlogits
+    return out
 
 
 class QkDesc:
@@ -499,12 +501,17 @@ def sp_qk_workspace_size(desc: QkDesc) -> int:
     return n.value
 
 
-def _heads(t, name, shape, dev, optional=False):
+def _heads(t, name, shape, dev):
     """Pointer and token stride of a [T, H, D] bf16 tensor whose tokens may lie
     further apart than their heads need."""
     import torch
-    p = _arg(t, name, torch.bfloat16, shape, dev, optional=optional, rows=True)
-    return p, (shape[1] * shape[2] if t is None or shape[0] < 2 else t.stride(0))
+    T, H, D = shape
+    if t is None or t.dtype is not torch.bfloat16 or t.shape != shape or t.get_device() != dev or T < 2:
+        return _arg(t, name, torch.bfloat16, shape, dev), H * D
+    st, sh, sd = t.stride()
+    if sd != 1 or (sh != D and H > 1):
+        raise ValueError(f"{name} must be contiguous within a token")
+    return t.data_ptr(), st
 
 
 def sp_qk_norm_rope(desc: QkDesc, q, k, v, positions=None, w_q=None, w_k=None, q_dst=None, k_dst=None, v_dst=None,
@@ -514,18 +521,15 @@ def sp_qk_norm_rope(desc: QkDesc, q, k, v, positions=None, w_q=None, w_k=None, q
     rotated by positions [T] int32 (None: position_base + t) and packed."""
     import torch
     c, dev, bf = desc.c, _device_of(stream), torch.bfloat16
-    T, D = c.T, c.head_dim
-    args = (*_heads(q, "q", (T, c.H_q, D), dev), *_heads(k, "k", (T, c.H_kv, D), dev),
-            *_heads(v, "v", (T, c.H_kv, D), dev), _arg(positions, "positions", torch.int32, (T,), dev, optional=True),
-            _arg(w_q, "w_q", bf, (D,), dev, optional=True), _arg(w_k, "w_k", bf, (D,), dev, optional=True))
+    T, D, Hq, Hkv = c.T, c.head_dim, c.H_q, c.H_kv
+    args = (*_heads(q, "q", (T, Hq, D), dev), *_heads(k, "k", (T, Hkv, D), dev), *_heads(v, "v", (T, Hkv, D), dev),
+            _arg(positions, "positions", torch.int32, (T,), dev, True), _arg(w_q, "w_q", bf, (D,), dev, True),
+            _arg(w_k, "w_k", bf, (D,), dev, True))
     sq, sk = (c.sp, T, c.Hq_loc, D), (c.sp, T, c.Hkv_loc, D)
     with _alloc_on(stream):
-        q_dst, k_dst, v_dst = (torch.empty(s, dtype=bf, device=q.device) if t is None else t
-                               for t, s in ((q_dst, sq), (k_dst, sk), (v_dst, sk)))
-        _check(load().sp_qk_norm_rope(desc.ref, *args, _arg(q_dst, "q_dst", bf, sq, dev),
-                                      _arg(k_dst, "k_dst", bf, sk, dev), _arg(v_dst, "v_dst", bf, sk, dev),
-                                      _stream(stream)), "sp_qk_norm_rope")
-    return q_dst, k_dst, v_dst
+        ts, ps = _outs([(q_dst, "q_dst", sq), (k_dst, "k_dst", sk), (v_dst, "v_dst", sk)], bf, q.device, dev)
+        _check(load().sp_qk_norm_rope(desc.ref, *args, *ps, _stream(stream)), "sp_qk_norm_rope")
+    return tuple(ts)
 
 
 def sp_qk_norm_rope_bwd(desc: QkDesc, q, k, dq_src, dk_src, dv_src, positions=None, w_q=None, w_k=None, dq=None,
@@ -535,28 +539,28 @@ def sp_qk_norm_rope_bwd(desc: QkDesc, q, k, dq_src, dk_src, dv_src, positions=No
     the weight).  q and k are needed where their weight is given."""
     import torch
     c, dev, bf, f = desc.c, _device_of(stream), torch.bfloat16, torch.float32
-    T, D = c.T, c.head_dim
+    T, D, Hq, Hkv = c.T, c.head_dim, c.H_q, c.H_kv
     sq, sk = (c.sp, T, c.Hq_loc, D), (c.sp, T, c.Hkv_loc, D)
-    hq, hk = (T, c.H_q, D), (T, c.H_kv, D)
-    args = (*_heads(q if w_q is not None else None, "q", hq, dev, optional=w_q is None),
-            *_heads(k if w_k is not None else None, "k", hk, dev, optional=w_k is None),
+    hq, hk = (T, Hq, D), (T, Hkv, D)
+    args = (*(_heads(q, "q", hq, dev) if w_q is not None else (None, 0)),
+            *(_heads(k, "k", hk, dev) if w_k is not None else (None, 0)),
             _arg(dq_src, "dq_src", bf, sq, dev), _arg(dk_src, "dk_src", bf, sk, dev),
-            _arg(dv_src, "dv_src", bf, sk, dev), _arg(positions, "positions", torch.int32, (T,), dev, optional=True),
-            _arg(w_q, "w_q", bf, (D,), dev, optional=True), _arg(w_k, "w_k", bf, (D,), dev, optional=True))
+            _arg(dv_src, "dv_src", bf, sk, dev), _arg(positions, "positions", torch.int32, (T,), dev, True),
+            _arg(w_q, "w_q", bf, (D,), dev, True), _arg(w_k, "w_k", bf, (D,), dev, True))
     for w, dw, name in ((w_q, dw_q, "dw_q"), (w_k, dw_k, "dw_k")):
         if w is None and dw is not None:
             raise ValueError(f"{name} is given without its weight")
+    device = dq_src.device
     with _alloc_on(stream):
-        dq, dk, dv = (torch.empty(s, dtype=bf, device=dq_src.device) if t is None else t
-                      for t, s in ((dq, hq), (dk, hk), (dv, hk)))
-        dw_q, dw_k = (torch.empty(D, dtype=f, device=dq_src.device) if dw is None and w is not None else dw
-                      for w, dw in ((w_q, dw_q), (w_k, dw_k)))
-        ws = _workspace(sp_qk_workspace_size(desc), workspace, dev)
+        dq, dk, dv = (torch.empty(s, dtype=bf, device=device) if t is None else t for t, s in ((dq, hq), (dk, hk), (dv, hk)))
+        dws, pws = _outs([(dw, n, (D,)) for w, dw, n in ((w_q, dw_q, "dw_q"), (w_k, dw_k, "dw_k")) if w is not None], f,
+                         device, dev)
+        ws = _workspace(sp_qk_workspace_size(desc), workspace, device, dev)
         _check(load().sp_qk_norm_rope_bwd(desc.ref, *args, *_heads(dq, "dq", hq, dev), *_heads(dk, "dk", hk, dev),
-                                          *_heads(dv, "dv", hk, dev), _arg(dw_q, "dw_q", f, (D,), dev, optional=True),
-                                          _arg(dw_k, "dw_k", f, (D,), dev, optional=True), ws.data_ptr(),
+                                          *_heads(dv, "dv", hk, dev), pws[0] if w_q is not None else None,
+                                          pws[-1] if w_k is not None else None, ws.data_ptr(),
                                           ws.numel() * ws.element_size(), _stream(stream)), "sp_qk_norm_rope_bwd")
-    return dq, dk, dv, dw_q, dw_k
+    return dq, dk, dv, dws[0] if w_q is not None else None, dws[-1] if w_k is not None else None
 
 
 def sp_attn_fwd(desc: Desc, q, k, v, o=None, lse=None, workspace=None, stream=None):

@@ -612,10 +612,10 @@ int slot_record(const sp_attn_desc* d, const Problem& p, const RowTile& t, size_
 }
 
 // Row items over such tiles; an item's first field is its tile's number until
-// place_records puts the records' place there.  Returns their steps, longest first.
+// place_records puts the records' place there.  Leaves `items` longest first and
+// returns their steps.
 Costs schedule_tiles(const sp_attn_desc* d, const Problem& p, const std::vector<RowTile>& tiles, int BN,
-                     std::vector<int32_t>& out, size_t n_front) {
-  std::vector<Item> items;
+                     std::vector<int32_t>& out, size_t n_front, std::vector<Item>& items) {
   std::vector<int> steps;
   for (const RowTile& t : tiles) steps.push_back(slot_record(d, p, t, 0, t.slots.size(), BN, kSlots, nullptr));
   for (int y = 0; y < p.n_real; ++y)
@@ -626,10 +626,10 @@ Costs schedule_tiles(const sp_attn_desc* d, const Problem& p, const std::vector<
 }
 
 // The records of every tile for launches that split its rows over `split`
-// workgroups; the items' first fields, from item `front` on, become the records'
-// places in a list where they start at int `base`.
+// workgroups; the row items' first fields become the records' places in a list where
+// they start at int `base`.
 std::vector<int32_t> place_records(const sp_attn_desc* d, const Problem& p, const std::vector<RowTile>& tiles, int split,
-                                   int BN, std::vector<int32_t>& items, size_t front, int base) {
+                                   int BN, std::vector<int32_t>& items, int base) {
   const int n = kSlots / split, ints = spk::record_ints(n);
   std::vector<int32_t> out((size_t)ints * split * tiles.size(), 0);
   for (size_t i = 0; i < tiles.size(); ++i)
@@ -638,24 +638,23 @@ std::vector<int32_t> place_records(const sp_attn_desc* d, const Problem& p, cons
       const size_t b = std::min<size_t>(tiles[i].slots.size(), a + n);
       slot_record(d, p, tiles[i], a, b, BN, n, &out[(i * split + w) * ints]);
     }
-  for (size_t i = front; i < items.size() / kItemInts; ++i)
-    items[i * kItemInts] = base + items[i * kItemInts] * split * ints;
+  for (size_t i = 0; i < items.size(); i += kItemInts)
+    if (items[i + 7] == 0) items[i] = base + items[i] * split * ints;
   return out;
 }
 // Either kind of row items.
 Costs schedule_row_items(const sp_attn_desc* d, const Problem& p, const std::vector<RowTile>& tiles, int BM, int BN,
-                         bool include_empty, std::vector<int32_t>& out, size_t n_front) {
+                         bool include_empty, std::vector<int32_t>& out, size_t n_front, std::vector<Item>& items) {
   return p.prefix.empty() ? schedule_rows(d, p, BM, BN, include_empty, out, n_front)
-                          : schedule_tiles(d, p, tiles, BN, out, n_front);
+                          : schedule_tiles(d, p, tiles, BN, out, n_front, items);
 }
 // Ints of the records under any split.
 size_t record_room(size_t n_tiles) { return n_tiles * 4 * (size_t)spk::record_ints(kSlots / 4); }
 
 // Key-tile items (dK / dV).  Every key of every real head gets exactly one
-// item.  Returns their steps, longest first.
+// item.  Leaves `items` longest first and returns their steps.
 Costs schedule_keys(const sp_attn_desc* d, const Problem& p, int BNK, int BQ,
-                    std::vector<int32_t>& out, size_t n_front) {
-  std::vector<Item> items;
+                    std::vector<int32_t>& out, size_t n_front, std::vector<Item>& items) {
   for (int y = 0; y < p.n_real; ++y) {
     for (const Seg& g : p.segs_k) {
       for (int a = g.ka; a < g.kb; a += BNK) {
@@ -673,6 +672,25 @@ Costs schedule_keys(const sp_attn_desc* d, const Problem& p, int BNK, int BQ,
   }
   sort_items(items, out, n_front, false);
   return costs_of(items);
+}
+
+// Row and key items of a backward in one launch as one list, longest first by the
+// model's time a step.  (Whole lists one after the other end with the second list's
+// longest items: 4 groups of a prompt and 8 answers, 20730 rows, 4 heads, dQ's behind
+// dK/dV's, 273 -> 255 us.)
+std::vector<int32_t> merged_items(const std::vector<Item>& rows, const std::vector<Item>& keys, size_t n_front) {
+  std::vector<Item> all;
+  for (const Item& x : rows) {
+    all.push_back(x);
+    all.back().cost = std::llrint((double)x.cost * kSplitDq.step * 1e3);
+  }
+  for (const Item& x : keys) {
+    all.push_back(x);
+    all.back().cost = std::llrint((double)x.cost * kSplitDkdv.step * 1e3);
+  }
+  std::vector<int32_t> out;
+  sort_items(all, out, n_front, false);
+  return out;
 }
 
 // Zero fills as work items of the same launch (no extra kernels): dummy
@@ -1001,15 +1019,12 @@ sp_status policy_args(const sp_policy_params* p, int32_t T, int32_t V, const int
                       entropy != nullptr, spk::policy_parts(T, V)};
   return SP_OK;
 }
-size_t policy_workspace(int32_t T, int32_t V) {
-  return std::max<size_t>(256, align256((size_t)T * spk::policy_parts(T, V) * 16));
-}
 }  // namespace
 
 sp_status sp_policy_workspace_size(int32_t T, int32_t V, size_t* bytes) {
   if (!bytes || T < 0 || V < 8 || V % 8 != 0) return SP_ERR_INVALID_ARG;
   if (T >= 1 << 24) return SP_ERR_UNSUPPORTED;
-  *bytes = policy_workspace(T, V);
+  *bytes = spk::policy_workspace(T, V);
   return SP_OK;
 }
 
@@ -1025,7 +1040,7 @@ sp_status sp_policy_loss(const sp_policy_params* params, const void* logits, con
   if (T > 0 && (!logits || !labels || !old_logp || !logp || !lse || !aligned16(logits))) return SP_ERR_INVALID_ARG;
   if (num_seqs > 0 && (!seq_sum || !seq_stats)) return SP_ERR_INVALID_ARG;
   if (T > 0 && num_seqs > 0 && !advantages) return SP_ERR_INVALID_ARG;
-  if (!workspace || workspace_bytes < policy_workspace(T, V) || ((uintptr_t)workspace & 255u) != 0)
+  if (!workspace || workspace_bytes < spk::policy_workspace(T, V) || ((uintptr_t)workspace & 255u) != 0)
     return SP_ERR_WORKSPACE;
   const spk::PolicyTokens tok{labels, old_logp, ref_logp, advantages, logp, lse, entropy};
   SP_HIP(spk::launch_policy_loss(a, k, logits, tok, workspace, seq_sum, seq_stats, (hipStream_t)stream));
@@ -1053,6 +1068,38 @@ sp_status sp_policy_loss_bwd(const sp_policy_params* params, const void* logits,
 }
 
 namespace {
+// radians / 2 pi in 2^-64 turns, whole turns dropped: the product as a sum of two
+// doubles, whose error is below 2^-104 of it.
+uint64_t turns64(double radians) {
+  constexpr double kInv = 0x1.45f306dc9c883p-3, kInvLow = -0x1.6b01ec5417056p-57;  // 1 / 2 pi
+  const double hi = radians * kInv, lo = std::fma(radians, kInv, -hi) + radians * kInvLow;
+  const double frac = hi - std::floor(hi);  // (exact, in [0, 1]: 1 for a tiny negative hi)
+  const uint64_t part = frac < 1.0 ? (uint64_t)(frac * 0x1p64) : 0;
+  const double low = std::fabs(lo) < 0.25 ? lo : std::fmod(lo, 0.25);
+  return part + (uint64_t)(int64_t)std::llrint(low * 0x1p64);
+}
+
+// The slots of a map in the order of their heads (ascending within a head, those
+// without one last), and where each head's begin; false for a bad entry.
+bool by_head(const int32_t* map, int sp, int H_loc, int H, uint32_t* slot, int* start) {
+  const int n = sp * H_loc;
+  int next[spk::kMaxQkHeads + 1] = {};
+  for (int i = 0; i < n; ++i) {
+    if (map[i] < -1 || map[i] >= H) return false;
+    if (map[i] >= 0) ++next[map[i]];
+  }
+  int at = 0;
+  for (int g = 0; g < H; ++g) {
+    start[g] = at;
+    at += next[g];
+    next[g] = start[g];
+  }
+  start[H] = next[H] = at;
+  for (int j = 0, i = 0; j < sp; ++j)
+    for (int h = 0; h < H_loc; ++h, ++i) slot[next[map[i] < 0 ? H : map[i]]++] = (uint32_t)h | (uint32_t)j << 10;
+  return true;
+}
+
 // Validation of a sp_qk_desc; fills the forward's kernel arguments.
 sp_status qk_args(const sp_qk_desc* d, spk::QkArgs& a) {
   if (!d) return SP_ERR_INVALID_ARG;
@@ -1071,42 +1118,18 @@ sp_status qk_args(const sp_qk_desc* d, spk::QkArgs& a) {
   a.rope_scale = d->rope_scale; a.eps = d->eps; a.w_off = d->weight_offset;
   for (int i = 0; i < d->rotary_dim / 2; ++i) {
     if (!std::isfinite(d->inv_freq[i])) return SP_ERR_INVALID_ARG;
-    // the fraction of a turn, in 2^-64: the long double has 64 bits for it
-    const long double turns = (long double)d->inv_freq[i] / 6.283185307179586476925286766559L;
-    const long double frac = turns - floorl(turns);
-    const long double fixed = roundl(frac * 18446744073709551616.0L);
-    a.freq[i] = fixed >= 18446744073709551616.0L ? 0 : (uint64_t)fixed;
+    a.freq[i] = turns64(d->inv_freq[i]);
   }
-  auto entries = [&](const int32_t* map, int H_loc, int H, uint32_t* slot) {
-    for (int i = 0; i < d->sp * H_loc; ++i) {
-      if (map[i] < -1 || map[i] >= H) return false;
-      slot[i] = (uint32_t)(i % H_loc) | (uint32_t)(i / H_loc) << 10 | (uint32_t)(map[i] + 1) << 20;
-    }
-    return true;
-  };
-  if (!entries(d->q_map, d->Hq_loc, d->H_q, a.q_slot) || !entries(d->kv_map, d->Hkv_loc, d->H_kv, a.kv_slot))
+  if (!by_head(d->q_map, d->sp, d->Hq_loc, d->H_q, a.q_slot, a.q_start) ||
+      !by_head(d->kv_map, d->sp, d->Hkv_loc, d->H_kv, a.kv_slot, a.kv_start))
     return SP_ERR_INVALID_ARG;
   return SP_OK;
-}
-// The entries of every head, ascending, in `slot` (which holds them by slot).
-void by_head(uint32_t* slot, int n, int H, int16_t* start) {
-  uint32_t sorted[spk::kMaxMap];
-  int at = 0;
-  for (int g = 0; g <= H; ++g) start[g] = 0;
-  for (int i = 0; i < n; ++i)
-    if (slot[i] >> 20) ++start[slot[i] >> 20];
-  for (int g = 0; g < H; ++g) start[g + 1] += start[g];
-  int16_t next[spk::kMaxQkHeads];
-  std::copy(start, start + H, next);
-  for (int i = 0; i < n; ++i)
-    if (slot[i] >> 20) sorted[next[(slot[i] >> 20) - 1]++] = slot[i], ++at;
-  std::copy(sorted, sorted + at, slot);
 }
 bool qk_stride_ok(const sp_qk_desc* d, int64_t stride, int H) {
   return stride % 8 == 0 && stride >= (int64_t)H * d->head_dim && stride < (int64_t(1) << 40);
 }
-size_t qk_workspace(const sp_qk_desc* d) {
-  return align256((size_t)spk::qk_bwd_groups(d->T) * 2 * d->head_dim * sizeof(float));
+size_t qk_workspace(const spk::QkArgs& a, int D) {
+  return align256((size_t)spk::qk_bwd_groups(a, D) * 2 * D * sizeof(float));
 }
 }  // namespace
 
@@ -1132,7 +1155,7 @@ sp_status sp_qk_workspace_size(const sp_qk_desc* d, size_t* bytes) {
   spk::QkArgs a;
   sp_status s = qk_args(d, a);
   if (s != SP_OK) return s;
-  *bytes = qk_workspace(d);
+  *bytes = qk_workspace(a, d->head_dim);
   return SP_OK;
 }
 
@@ -1141,8 +1164,8 @@ sp_status sp_qk_norm_rope_bwd(const sp_qk_desc* d, const void* q, int64_t q_stri
                               const void* w_q, const void* w_k, void* dq, int64_t dq_stride, void* dk, int64_t dk_stride,
                               void* dv, int64_t dv_stride, float* dw_q, float* dw_k, void* ws, size_t ws_bytes,
                               void* stream) {
-  spk::QkBwdArgs b{};
-  sp_status s = qk_args(d, b.a);
+  spk::QkArgs a{};
+  sp_status s = qk_args(d, a);
   if (s != SP_OK) return s;
   if (!qk_stride_ok(d, dq_stride, d->H_q) || !qk_stride_ok(d, dk_stride, d->H_kv) || !qk_stride_ok(d, dv_stride, d->H_kv) ||
       (w_q && !qk_stride_ok(d, q_stride, d->H_q)) || (w_k && !qk_stride_ok(d, k_stride, d->H_kv)))
@@ -1154,12 +1177,10 @@ sp_status sp_qk_norm_rope_bwd(const sp_qk_desc* d, const void* q, int64_t q_stri
     if ((w_q && !q) || (w_k && !k)) return SP_ERR_INVALID_ARG;
     if (!aligned16(q) || !aligned16(k) || !aligned16(w_q) || !aligned16(w_k)) return SP_ERR_INVALID_ARG;
   }
-  if (!ws || ws_bytes < qk_workspace(d) || ((uintptr_t)ws & 255u) != 0) return SP_ERR_WORKSPACE;
-  b.a.sq = q_stride / 8; b.a.sk = k_stride / 8;
-  b.dsq = dq_stride / 8; b.dsk = dk_stride / 8; b.dsv = dv_stride / 8;
-  by_head(b.a.q_slot, d->sp * d->Hq_loc, d->H_q, b.q_start);
-  by_head(b.a.kv_slot, d->sp * d->Hkv_loc, d->H_kv, b.kv_start);
-  SP_HIP(spk::launch_qk_rope_bwd(b, d->head_dim, q, k, dq_src, dk_src, dv_src, positions, w_q, w_k, dq, dk, dv, dw_q, dw_k,
+  if (!ws || ws_bytes < qk_workspace(a, d->head_dim) || ((uintptr_t)ws & 255u) != 0) return SP_ERR_WORKSPACE;
+  a.sq = q_stride / 8; a.sk = k_stride / 8;
+  const spk::QkStrides o{dq_stride / 8, dk_stride / 8, dv_stride / 8};
+  SP_HIP(spk::launch_qk_rope_bwd(a, o, d->head_dim, q, k, dq_src, dk_src, dv_src, positions, w_q, w_k, dq, dk, dv, dw_q, dw_k,
                                  w_q || w_k ? (float*)ws : nullptr, (hipStream_t)stream));
   return SP_OK;
 }
@@ -1184,13 +1205,14 @@ sp_status sp_attn_schedule(const sp_attn_desc* desc, int32_t op, int32_t* items,
   sp_status s = validate(desc, p);
   if (s != SP_OK) return s;
   std::vector<int32_t> v;
+  std::vector<Item> items_;
   // in launch order: the fill items that precede the listed ones there
   // shift the workgroup -> XCD map
   if ((op == SP_OP_FWD || op == SP_OP_RING_STEP) && !p.prefix.empty()) {
     if (op == SP_OP_RING_STEP) return SP_ERR_UNSUPPORTED;
     const std::vector<RowTile> tiles = row_tiles(desc, p);
     std::vector<int32_t> it;
-    schedule_tiles(desc, p, tiles, spk::kFwdBN, it, row_fills(desc, p).size() / kItemInts);
+    schedule_tiles(desc, p, tiles, spk::kFwdBN, it, row_fills(desc, p).size() / kItemInts, items_);
     for (size_t i = 0; i < it.size(); i += kItemInts) {  // slot by slot
       const RowTile& t = tiles[it[i]];
       for (const spk::RowSlot& s : t.slots) {
@@ -1204,7 +1226,7 @@ sp_status sp_attn_schedule(const sp_attn_desc* desc, int32_t op, int32_t* items,
     schedule_rows(desc, p, spk::kFwdBM, spk::kFwdBN, true, v,
                   row_fills(desc, p).size() / kItemInts);
   else if (op == SP_OP_BWD)
-    schedule_keys(desc, p, spk::kDkdvBN, spk::kDkdvBQ, v, key_fills(desc, p).size() / kItemInts);
+    schedule_keys(desc, p, spk::kDkdvBN, spk::kDkdvBQ, v, key_fills(desc, p).size() / kItemInts, items_);
   else
     return SP_ERR_INVALID_ARG;
   const int32_t n = (int32_t)(v.size() / kItemInts);
@@ -1222,14 +1244,16 @@ sp_status sp_attn_plan(const sp_attn_desc* desc, int32_t op, int32_t* plan) {
   if (op == SP_OP_RING_STEP && !p.prefix.empty()) return SP_ERR_UNSUPPORTED;
   const std::vector<RowTile> tiles = p.prefix.empty() ? std::vector<RowTile>() : row_tiles(desc, p);
   std::vector<int32_t> v;
+  std::vector<Item> rows;
   BwdPlan b{};
   if (op == SP_OP_BWD) {
-    const Costs q = schedule_row_items(desc, p, tiles, spk::kDqBM, spk::kDqBN, true, v, 0);
-    const Costs k = schedule_keys(desc, p, spk::kDkdvBN, spk::kDkdvBQ, v, 0);
+    std::vector<Item> keys;
+    const Costs q = schedule_row_items(desc, p, tiles, spk::kDqBM, spk::kDqBN, true, v, 0, rows);
+    const Costs k = schedule_keys(desc, p, spk::kDkdvBN, spk::kDkdvBQ, v, 0, keys);
     b = plan_bwd(q, k, p.D);
   } else {
     double us;
-    b.q = choose_shape(schedule_row_items(desc, p, tiles, spk::kFwdBM, spk::kFwdBN, true, v, 0), kSplitFwd,
+    b.q = choose_shape(schedule_row_items(desc, p, tiles, spk::kFwdBM, spk::kFwdBN, true, v, 0, rows), kSplitFwd,
                        p.D, us);
   }
   const int32_t r[SP_PLAN_INTS] = {b.q.split, b.q.two, b.k.split, b.k.two, b.one, b.dq_first};
@@ -1310,16 +1334,16 @@ static sp_status fwd_common(const sp_attn_desc* d, const void* q, const void* k,
   std::vector<int32_t> items;
   const std::vector<int32_t> fills = include_empty ? row_fills(d, p) : std::vector<int32_t>();
   const std::vector<RowTile> tiles = prefix ? row_tiles(d, p) : std::vector<RowTile>();
+  std::vector<Item> rows;
   const Costs cost = schedule_row_items(d, p, tiles, spk::kFwdBM, spk::kFwdBN, include_empty, items,
-                                        fills.size() / kItemInts);
+                                        fills.size() / kItemInts, rows);
   prepend(fills, items);
   const int n_items = (int)(items.size() / kItemInts);
   double us;
   const spk::LaunchShape shape = choose_shape(cost, kSplitFwd, p.D, us);
   if (prefix) {
     const std::vector<int32_t> records =
-        place_records(d, p, tiles, shape.split, spk::fwd_tile_keys(p.D, shape.split), items, fills.size() / kItemInts,
-                      (int)items.size());
+        place_records(d, p, tiles, shape.split, spk::fwd_tile_keys(p.D, shape.split), items, (int)items.size());
     items.insert(items.end(), records.begin(), records.end());
   }
   hipStream_t st = (hipStream_t)stream;
@@ -1409,11 +1433,12 @@ sp_status sp_attn_bwd(const sp_attn_desc* d, const void* q, const void* k, const
   const std::vector<int32_t> fkv = key_fills(d, p);
   const bool prefix = !p.prefix.empty();
   const std::vector<RowTile> tiles = prefix ? row_tiles(d, p) : std::vector<RowTile>();
+  std::vector<Item> rows, keys;
   const Costs cost_q =
-      schedule_row_items(d, p, tiles, spk::kDqBM, spk::kDqBN, true, it_dq, fq.size() / kItemInts);
+      schedule_row_items(d, p, tiles, spk::kDqBM, spk::kDqBN, true, it_dq, fq.size() / kItemInts, rows);
   prepend(fq, it_dq);
   const Costs cost_k =
-      schedule_keys(d, p, spk::kDkdvBN, spk::kDkdvBQ, it_kv, fkv.size() / kItemInts);
+      schedule_keys(d, p, spk::kDkdvBN, spk::kDkdvBQ, it_kv, fkv.size() / kItemInts, keys);
   prepend(fkv, it_kv);
   const size_t na = it_dq.size() / kItemInts, nb = it_kv.size() / kItemInts;
   // (the records of row tiles lie behind the dQ items, or in a launch's own list
@@ -1424,12 +1449,24 @@ sp_status sp_attn_bwd(const sp_attn_desc* d, const void* q, const void* k, const
   if ((s = refuse_capture(st)) != SP_OK) return s;
   const int D = p.D;
   const BwdPlan plan = plan_bwd(cost_q, cost_k, D);
+  // dK, dV written over K, V: a key's rows are read and written by one dK/dV
+  // workgroup, but dQ reads all of them, so it ends first (same splits, same
+  // bits)
+  const bool over_kv = dk == k || dk == v || dv == k || dv == v;
+  // one list where its items are whole (it takes the place of dQ's)
+  const bool merged = prefix && plan.one && !over_kv && plan.q.split == 1 && plan.k.split == 1;
+  if (merged) {
+    it_dq = merged_items(rows, keys, (fq.size() + fkv.size()) / kItemInts);
+    prepend(fkv, it_dq);
+    prepend(fq, it_dq);
+    it_kv.clear();
+  }
   const size_t n_rec = tiles.size() * plan.q.split * spk::record_ints(kSlots / plan.q.split);
   const bool by_value = it_dq.size() + it_kv.size() + n_rec <= std::size(spk::ItemList().v);
   const size_t rec_at = by_value ? it_dq.size() + it_kv.size() : it_dq.size();
   std::vector<int32_t> records;
   if (prefix)
-    records = place_records(d, p, tiles, plan.q.split, spk::kDqBN, it_dq, fq.size() / kItemInts, (int)rec_at);
+    records = place_records(d, p, tiles, plan.q.split, spk::kDqBN, it_dq, (int)rec_at);
   {
     // Work lists that fit a launch's arguments go there (a launch of its own
     // for dK/dV has its list first).  Else both in one copy (they are adjacent
@@ -1439,7 +1476,7 @@ sp_status sp_attn_bwd(const sp_attn_desc* d, const void* q, const void* k, const
     if (by_value) {
       std::copy(records.begin(), records.end(), list.v + rec_at);
     } else {
-      const size_t gap = (L.items_kv - L.items_dq) / sizeof(int32_t);
+      const size_t gap = merged ? rec_at + n_rec : (L.items_kv - L.items_dq) / sizeof(int32_t);
       std::vector<int32_t> both(gap + it_kv.size(), 0);
       std::copy(it_dq.begin(), it_dq.end(), both.begin());
       std::copy(records.begin(), records.end(), both.begin() + rec_at);
@@ -1459,7 +1496,7 @@ sp_status sp_attn_bwd(const sp_attn_desc* d, const void* q, const void* k, const
     a.items = by_value ? nullptr : (const int32_t*)at(ws, L.items_dq);
     a.T_q = d->T_q; a.T_k = d->T_k; a.H = d->H_loc; a.Hkv = d->Hkv_loc;
     a.scale_log2 = sl2; a.scale = d->softmax_scale; a.causal = d->causal;
-    a.n_items = (int)na;
+    a.n_items = (int)(it_dq.size() / kItemInts);
 
     spk::DkdvArgs b{};
     b.q = (const uint16_t*)q;
@@ -1471,15 +1508,12 @@ sp_status sp_attn_bwd(const sp_attn_desc* d, const void* q, const void* k, const
     b.items = by_value ? nullptr : (const int32_t*)at(ws, L.items_kv);
     b.T_q = d->T_q; b.T_k = d->T_k; b.H = d->H_loc; b.Hkv = d->Hkv_loc;
     b.scale_log2 = sl2; b.scale = d->softmax_scale; b.causal = d->causal; b.direct = p.direct;
-    b.n_items = (int)nb;
+    b.n_items = merged ? a.n_items : (int)nb;
+    if (merged) b.items = a.items;
     if (by_value) std::copy(it_dq.begin(), it_dq.end(), list.v);
-    // dK, dV written over K, V: a key's rows are read and written by one dK/dV
-    // workgroup, but dQ reads all of them, so it ends first (same splits, same
-    // bits)
-    const bool over_kv = dk == k || dk == v || dv == k || dv == v;
     if (plan.one && !over_kv) {
       if (by_value) std::copy(it_kv.begin(), it_kv.end(), list.v + it_dq.size());
-      SP_HIP(spk::launch_attn_bwd(a, b, list, plan.q, plan.k, plan.dq_first, D, prefix, st));
+      SP_HIP(spk::launch_attn_bwd(a, b, list, plan.q, plan.k, plan.dq_first, D, prefix, merged, st));
     } else {
       SP_HIP(spk::launch_attn_dq(a, list, plan.q, D, prefix, st));
       if (by_value) std::copy(it_kv.begin(), it_kv.end(), list.v);

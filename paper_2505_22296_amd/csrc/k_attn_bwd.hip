@@ -702,6 +702,16 @@ __global__ __launch_bounds__(NTQ, TWO ? 4 : 1) void attn_bwd_kernel(DqArgs a, Dk
   using Q = DqStage<D, KW>;
   using K = DkdvStage<D, TWO>;
   __shared__ u32x4 smem[Q::SMEM > K::SMEM ? Q::SMEM : K::SMEM];
+  if constexpr (PFX && KW == 1 && RG == 1) {
+    if (n_first < 0) {  // one list of both kinds
+      const int kind = table_at(a.items, list, blockIdx.x * kItemInts + 7);
+      if (kind == 0 || kind == kItemFillQ)
+        dq_body<D, KW, TWO, PFX>(a, list, smem, blockIdx.x);
+      else
+        dkdv_wg<D, RG, TWO>(b, list, 0, smem, blockIdx.x);
+      return;
+    }
+  }
   const bool first = (int)blockIdx.x < n_first;
   const int block = first ? blockIdx.x : blockIdx.x - n_first;
   if (first == (dq_first != 0))
@@ -751,7 +761,12 @@ hipError_t launch_attn_dkdv(const DkdvArgs& a, const ItemList& list, LaunchShape
 
 template <int D, int KW, int RG, bool TWO>
 static hipError_t launch_bwd(const DqArgs& a, const DkdvArgs& b, const ItemList& list,
-                             bool dq_first, bool prefix, hipStream_t st) {
+                             bool dq_first, bool prefix, bool merged, hipStream_t st) {
+  if (merged) {
+    if (!prefix || KW != 1 || RG != 1) return hipErrorInvalidValue;
+    return sp_launch2(kKDq, kKDkdv, attn_bwd_kernel<D, KW, RG, TWO, true>, dim3(a.n_items), dim3(NTQ), st, a, b, list,
+                      -1, 0);
+  }
   // the first list's workgroups are rounded up to eight, so that the second
   // list's positions keep their XCDs
   const int nq = split_grid(a.n_items, KW), nk = split_grid(b.n_items, RG);
@@ -762,21 +777,21 @@ static hipError_t launch_bwd(const DqArgs& a, const DkdvArgs& b, const ItemList&
 }
 
 hipError_t launch_attn_bwd(const DqArgs& a, const DkdvArgs& b, const ItemList& list, LaunchShape q,
-                           LaunchShape k, bool dq_first, int D, bool prefix, hipStream_t st) {
+                           LaunchShape k, bool dq_first, int D, bool prefix, bool merged, hipStream_t st) {
   if (D == 128) {
     if (q.split == 4 && k.split == 2)
-      return launch_bwd<128, 4, 2, false>(a, b, list, dq_first, prefix, st);
+      return launch_bwd<128, 4, 2, false>(a, b, list, dq_first, prefix, merged, st);
     if (q.split == 2 && k.split == 1)
-      return launch_bwd<128, 2, 1, false>(a, b, list, dq_first, prefix, st);
+      return launch_bwd<128, 2, 1, false>(a, b, list, dq_first, prefix, merged, st);
     if (q.split == 1 && k.split == 1)
-      return launch_bwd<128, 1, 1, false>(a, b, list, dq_first, prefix, st);
+      return launch_bwd<128, 1, 1, false>(a, b, list, dq_first, prefix, merged, st);
     return hipErrorInvalidValue;
   }
-  if (q.split == 4 && k.split == 2) return launch_bwd<64, 4, 2, false>(a, b, list, dq_first, prefix, st);
-  if (q.split == 2 && k.split == 1) return launch_bwd<64, 2, 1, false>(a, b, list, dq_first, prefix, st);
+  if (q.split == 4 && k.split == 2) return launch_bwd<64, 4, 2, false>(a, b, list, dq_first, prefix, merged, st);
+  if (q.split == 2 && k.split == 1) return launch_bwd<64, 2, 1, false>(a, b, list, dq_first, prefix, merged, st);
   if (q.split == 1 && k.split == 1)
-    return q.two ? launch_bwd<64, 1, 1, true>(a, b, list, dq_first, prefix, st)
-                 : launch_bwd<64, 1, 1, false>(a, b, list, dq_first, prefix, st);
+    return q.two ? launch_bwd<64, 1, 1, true>(a, b, list, dq_first, prefix, merged, st)
+                 : launch_bwd<64, 1, 1, false>(a, b, list, dq_first, prefix, merged, st);
   return hipErrorInvalidValue;
 }
 

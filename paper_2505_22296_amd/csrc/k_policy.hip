@@ -44,8 +44,11 @@ SP_DEV RowSum join(const RowSum& p, const RowSum& q) {
                 wp * __builtin_fmaf(p.s, dp, p.u) + wq * __builtin_fmaf(q.s, dq, q.u)};
 }
 
-// N chunks of eight logits into the running sums.
-template <int N, bool ENT>
+// N chunks of eight logits into the running sums.  MASKED: logits of -inf and of
+// the type's lowest value, whose y is -inf, add 0 to u (else NaN: see row_sums).
+// The maximum is the one that passes NaN on (one instruction for three operands;
+// fmaxf first quiets each).
+template <int N, bool ENT, bool MASKED>
 SP_DEV void add_chunks(RowSum& r, const u32x4 (&v)[N]) {
   float x[8 * N];
   float top = neg_inf();
@@ -55,15 +58,15 @@ SP_DEV void add_chunks(RowSum& r, const u32x4 (&v)[N]) {
     for (int k = 0; k < 4; ++k) {
       x[8 * c + 2 * k] = __uint_as_float(v[c][k] << 16);
       x[8 * c + 2 * k + 1] = __uint_as_float(v[c][k] & 0xffff0000u);
-      top = fmaxf(fmaxf(top, x[8 * c + 2 * k]), x[8 * c + 2 * k + 1]);
+      top = max3_nonan(top, x[8 * c + 2 * k], x[8 * c + 2 * k + 1]);
     }
-  const float b = fmaxf(r.b, top * kLog2e);
+  const float b = __builtin_elementwise_maximum(r.b, top * kLog2e);
   const float d = r.b - b, w = __builtin_amdgcn_exp2f(d);
   float s = w * r.s, u = w * __builtin_fmaf(r.s, d, r.u);
 #pragma unroll
   for (int i = 0; i < 8 * N; ++i) {
     float y = __builtin_fmaf(x[i], kLog2e, -b);
-    if constexpr (ENT) y = fmaxf(y, kLowest);  // a logit of -inf: 2^y = 0, and 2^y y too
+    if constexpr (ENT && MASKED) y = fmaxf(y, kLowest);
     const float e = __builtin_amdgcn_exp2f(y);
     s += e;
     if constexpr (ENT) u = __builtin_fmaf(e, y, u);
@@ -127,97 +130,53 @@ SP_DEV TokenTerms token_terms(const PolicyArgs& p, const RowSum& r, uint16_t lab
   return o;
 }
 
-// A workgroup sums one part of one row's vocabulary; WHOLE: the row, and its
-// first thread writes what the token contributes (beside other workgroups' loads;
-// the sums' few workgroups would take longer over it).  `part`: the parts' sums, or
-// {term, kl, entropy, clipped} of every token.
-template <bool ENT, bool WHOLE>
-__global__ __launch_bounds__(kPB) void policy_rows_kernel(LossArgs a, PolicyArgs p, const u32x4* __restrict__ logits,
-                                                          PolicyTokens tok, f32x4* __restrict__ part) {
-  const int t = WHOLE ? blockIdx.x : blockIdx.x / p.parts, j = WHOLE ? 0 : blockIdx.x - t * p.parts;
-  const int label = tok.labels[t], seq = seq_of(a, t);
-  if (!label_counts(a, label) || seq < 0) {
-    if (WHOLE && threadIdx.x == 0) {
-      tok.logp[t] = 0.f;
-      tok.lse[t] = 0.f;
-      if (ENT) tok.ent[t] = 0.f;
-    }
-    return;
-  }
-  const int nch = a.V / 8;
-  const int c0 = WHOLE ? 0 : (int)((int64_t)nch * j / p.parts);
-  const int c1 = WHOLE ? nch : (int)((int64_t)nch * (j + 1) / p.parts);
-  const u32x4* row = logits + (int64_t)t * nch;
+// The sums of chunks [c0, c1) of a row by a workgroup, on all its threads.
+template <bool ENT, bool MASKED>
+SP_DEV RowSum row_sums(const u32x4* row, int c0, int c1, RowSum* sw) {
   RowSum r{kLowest, 0.f, 0.f};
-  int c = c0 + threadIdx.x;
-  for (; c + (kPU - 1) * kPB < c1; c += kPU * kPB) {
+  for (int c = c0 + threadIdx.x; c < c1; c += kPU * kPB) {
     u32x4 v[kPU];
 #pragma unroll
-    for (int i = 0; i < kPU; ++i) v[i] = ld_stream(&row[c + i * kPB]);
-    add_chunks<kPU, ENT>(r, v);
-  }
-  for (; c < c1; c += kPB) {
-    const u32x4 v[1] = {ld_stream(&row[c])};
-    add_chunks<1, ENT>(r, v);
+    for (int i = 0; i < kPU; ++i)  // (past the end: -1e38, which weighs nothing and keeps y finite)
+      v[i] = c + i * kPB < c1 ? ld_stream(&row[c + i * kPB]) : u32x4{0xfe96fe96u, 0xfe96fe96u, 0xfe96fe96u, 0xfe96fe96u};
+    add_chunks<kPU, ENT, MASKED>(r, v);
   }
 #pragma unroll
   for (int off = 32; off >= 1; off >>= 1)
     r = join(r, RowSum{__shfl_xor(r.b, off), __shfl_xor(r.s, off), __shfl_xor(r.u, off)});
-  __shared__ RowSum sw[kPB / 64];
   if ((threadIdx.x & 63) == 0) sw[threadIdx.x >> 6] = r;
   __syncthreads();
-  if (threadIdx.x == 0) {
 #pragma unroll
-    for (int i = 1; i < kPB / 64; ++i) r = join(r, sw[i]);
-    if constexpr (WHOLE) {
-      const TokenTerms o = token_terms(p, r, ((const uint16_t*)row)[label], tok, t, seq);
-      part[t] = f32x4{(float)o.term, (float)o.kl, o.ent, o.clipped};
-    } else {
-      part[(int64_t)t * p.parts + j] = f32x4{r.b, r.s, r.u, 0.f};
-    }
-  }
+  for (int i = 0; i < kPB / 64; ++i) r = i ? join(r, sw[i]) : sw[0];
+  return r;
 }
 
-// One workgroup of B threads a sequence: sums what its tokens contribute, in a
-// fixed order and 64 bits.  JOIN: it joins the parts of the tokens' rows first
-// (few tokens); the first and the last workgroup then also write the tokens
-// outside every sequence.
-template <int B, bool JOIN>
-__global__ __launch_bounds__(B) void policy_sums_kernel(LossArgs a, PolicyArgs p, const uint16_t* __restrict__ logits,
-                                                        PolicyTokens tok, const f32x4* __restrict__ part,
-                                                        float* __restrict__ seq_sum, float* __restrict__ stats) {
-  const int s = blockIdx.x;
-  const int b = a.n_seqs ? a.cu[s] : 0, e = a.n_seqs ? a.cu[s + 1] : 0;
-  const int t0 = JOIN && s == 0 ? 0 : b, t1 = JOIN && s + 1 >= a.n_seqs ? a.T : e;
-  double acc[5] = {0, 0, 0, 0, 0};  // term, kl, entropy, clipped, tokens
-  for (int t = t0 + threadIdx.x; t < t1; t += B) {
-    const int label = tok.labels[t];
-    if (t < b || t >= e || !label_counts(a, label)) {
-      if constexpr (JOIN) {
-        tok.logp[t] = 0.f;
-        tok.lse[t] = 0.f;
-        if (p.entropy) tok.ent[t] = 0.f;
-      }
-      continue;
-    }
-    if constexpr (JOIN) {
-      const f32x4* q = part + (int64_t)t * p.parts;
-      RowSum r{q[0][0], q[0][1], q[0][2]};
-      for (int i = 1; i < p.parts; ++i) r = join(r, RowSum{q[i][0], q[i][1], q[i][2]});
-      const TokenTerms o = token_terms(p, r, logits[(int64_t)t * a.V + label], tok, t, s);
-      acc[0] += o.term;
-      acc[1] += o.kl;
-      acc[2] += (double)o.ent;
-      acc[3] += (double)o.clipped;
-    } else {
-      const f32x4 o = part[t];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) acc[i] += (double)o[i];
-    }
-    acc[4] += 1.0;
+// A workgroup sums one part of one row's vocabulary.  (The token's values formed
+// here by the first thread, a workgroup a row: 145 instead of 137 us for 2800 counted
+// rows of 152064 logits.)
+template <bool ENT>
+__global__ __launch_bounds__(kPB) void policy_rows_kernel(LossArgs a, PolicyArgs p, const u32x4* __restrict__ logits,
+                                                          const int32_t* __restrict__ labels,
+                                                          f32x4* __restrict__ part) {
+  const int t = blockIdx.x / p.parts, j = blockIdx.x - t * p.parts;
+  if (!label_counts(a, labels[t]) || seq_of(a, t) < 0) return;
+  __shared__ RowSum sw[kPB / 64];
+  const int nch = a.V / 8;
+  const int c0 = (int)((int64_t)nch * j / p.parts), c1 = (int)((int64_t)nch * (j + 1) / p.parts);
+  const u32x4* row = logits + (int64_t)t * nch;
+  RowSum r = row_sums<ENT, false>(row, c0, c1, sw);
+  // 2^y y of a masked logit is NaN in u alone: such a row is gone through once more
+  // with y bounded (a row without masked logits saves that operation a logit)
+  if (ENT && r.u != r.u && r.s == r.s) {
+    __syncthreads();
+    r = row_sums<ENT, true>(row, c0, c1, sw);
   }
-  if (a.n_seqs == 0) return;
-  __shared__ double red[B / 64][5];
+  if (threadIdx.x == 0) part[(int64_t)t * p.parts + j] = f32x4{r.b, r.s, r.u, 0.f};
+}
+
+// Sum of five values over a workgroup in a fixed order; x[i] on thread i.
+SP_DEV double sum5(double (&acc)[5]) {
+  __shared__ double red[kPB / 64][5];
 #pragma unroll
   for (int i = 0; i < 5; ++i) {
 #pragma unroll
@@ -225,14 +184,73 @@ __global__ __launch_bounds__(B) void policy_sums_kernel(LossArgs a, PolicyArgs p
     if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6][i] = acc[i];
   }
   __syncthreads();
-  if (threadIdx.x < 5) {
-    double x = red[0][threadIdx.x];
-    for (int w = 1; w < B / 64; ++w) x += red[w][threadIdx.x];
-    if (threadIdx.x == 0)
-      seq_sum[s] = (float)x;
-    else
-      stats[s * 4 + threadIdx.x - 1] = (float)x;
+  double x = 0.0;
+  if (threadIdx.x < 5)
+    for (int w = 0; w < kPB / 64; ++w) x += red[w][threadIdx.x];
+  return x;
+}
+SP_DEV void write_sums(int s, double x, float* seq_sum, float* stats) {
+  if (threadIdx.x == 0)
+    seq_sum[s] = (float)x;
+  else if (threadIdx.x < 5)
+    stats[s * 4 + threadIdx.x - 1] = (float)x;
+}
+
+// One workgroup for kSumTokens tokens of a sequence (blockIdx.y of blockIdx.x): joins
+// the parts of their rows, writes what the tokens contribute and sums it in a fixed
+// order and 64 bits, for a sequence of one workgroup to the outputs, else to
+// `partial` [n_seqs, gridDim.y, 5].  The first workgroup of the first and of the last
+// sequence also write the tokens outside every sequence.
+constexpr int kSumTokens = 4 * kPB;
+__global__ __launch_bounds__(kPB) void policy_sums_kernel(LossArgs a, PolicyArgs p, const uint16_t* __restrict__ logits,
+                                                          PolicyTokens tok, const f32x4* __restrict__ part,
+                                                          double* __restrict__ partial, float* __restrict__ seq_sum,
+                                                          float* __restrict__ stats) {
+  const int s = blockIdx.x;
+  const int b = a.n_seqs ? a.cu[s] : 0, e = a.n_seqs ? a.cu[s + 1] : 0;
+  auto zero = [&](int t) {
+    tok.logp[t] = 0.f;
+    tok.lse[t] = 0.f;
+    if (p.entropy) tok.ent[t] = 0.f;
+  };
+  if (blockIdx.y == 0) {
+    if (s == 0)
+      for (int t = threadIdx.x; t < b; t += kPB) zero(t);
+    if (s + 1 >= a.n_seqs)
+      for (int t = e + threadIdx.x; t < a.T; t += kPB) zero(t);
   }
+  double acc[5] = {0, 0, 0, 0, 0};  // term, kl, entropy, clipped, tokens
+  const int t0 = b + blockIdx.y * kSumTokens, t1 = min(e, t0 + kSumTokens);
+  for (int t = t0 + threadIdx.x; t < t1; t += kPB) {
+    const int label = tok.labels[t];
+    if (!label_counts(a, label)) {
+      zero(t);
+      continue;
+    }
+    const f32x4* q = part + (int64_t)t * p.parts;
+    RowSum r{q[0][0], q[0][1], q[0][2]};
+    for (int i = 1; i < p.parts; ++i) r = join(r, RowSum{q[i][0], q[i][1], q[i][2]});
+    const TokenTerms o = token_terms(p, r, logits[(int64_t)t * a.V + label], tok, t, s);
+    acc[0] += o.term;
+    acc[1] += o.kl;
+    acc[2] += (double)o.ent;
+    acc[3] += (double)o.clipped;
+    acc[4] += 1.0;
+  }
+  if (a.n_seqs == 0) return;
+  const double x = sum5(acc);
+  if (gridDim.y == 1)
+    write_sums(s, x, seq_sum, stats);
+  else if (threadIdx.x < 5)
+    partial[((int64_t)s * gridDim.y + blockIdx.y) * 5 + threadIdx.x] = x;
+}
+__global__ __launch_bounds__(kPB) void policy_join_kernel(const double* __restrict__ partial, int n,
+                                                          float* __restrict__ seq_sum, float* __restrict__ stats) {
+  double acc[5] = {0, 0, 0, 0, 0};
+  for (int i = threadIdx.x; i < n; i += kPB)
+#pragma unroll
+    for (int k = 0; k < 5; ++k) acc[k] += partial[((int64_t)blockIdx.x * n + i) * 5 + k];
+  write_sums(blockIdx.x, sum5(acc), seq_sum, stats);
 }
 
 // A workgroup takes kPU loads a thread of one row (few rows fill the chip too,
@@ -287,7 +305,10 @@ __global__ __launch_bounds__(kPB) void policy_bwd_kernel(LossArgs a, PolicyArgs 
       } else {
         d[k] = e * k0;
       }
-      if (c * 8 + k == label) d[k] += g;
+    }
+    if (c == label >> 3) {  // (one lane of one workgroup a row)
+#pragma unroll
+      for (int k = 0; k < 8; ++k) d[k] += (label & 7) == k ? g : 0.f;
     }
     st_stream(pack_bf16x8(d[0], d[1], d[2], d[3], d[4], d[5], d[6], d[7]), &dlogits[base + c]);
   }
@@ -295,30 +316,38 @@ __global__ __launch_bounds__(kPB) void policy_bwd_kernel(LossArgs a, PolicyArgs 
 
 }  // namespace
 
-// Parts of a row in the forward: one where the rows fill the chip, else as many
-// as give each workgroup one round of loads.
+// Parts of a row in the forward.  Few rows: as many as give 2048 workgroups, down to
+// one round of loads each.  Else four rounds each: rows end on a CU one after the
+// other, and the last ones sooner (2800 rows of 152064 logits in 1 / 2 / 4 / 8 / 18
+// parts: 145 / 137 / 137 / 139 / 166 us).
 int policy_parts(int T, int V) {
-  const int nch = V / 8;
-  const int most = std::max(1, nch / (kPB * kPU));
-  return std::min(most, std::max(1, 2048 / std::max(T, 1)));
+  const int most = std::max(1, V / 8 / (kPB * kPU));
+  return std::min(most, std::max({1, most / 4, 2048 / std::max(T, 1)}));
+}
+// Workspace: the parts' sums, then the sums of long sequences' pieces (at most one
+// for every kSumTokens tokens and one a sequence).
+size_t policy_partial_at(int T, int V) { return ((size_t)T * policy_parts(T, V) * 16 + 255) & ~size_t(255); }
+size_t policy_workspace(int T, int V) {
+  return policy_partial_at(T, V) + ((size_t)(T / kSumTokens + 1) * kMaxLossSeqs * 5 * sizeof(double) + 255 & ~size_t(255));
 }
 
 hipError_t launch_policy_loss(const LossArgs& a, const PolicyArgs& p, const void* logits, const PolicyTokens& tok,
-                              void* part, float* seq_sum, float* stats, hipStream_t st) {
-  if (a.T > 0 && (a.n_seqs > 0 || p.parts == 1)) {
-    auto* kernel = p.parts == 1 ? (p.entropy ? policy_rows_kernel<true, true> : policy_rows_kernel<false, true>)
-                                : (p.entropy ? policy_rows_kernel<true, false> : policy_rows_kernel<false, false>);
-    hipError_t e = sp_launch(kKPolicy, kernel, dim3((unsigned)a.T * p.parts), dim3(kPB), st, a, p, (const u32x4*)logits,
-                             tok, (f32x4*)part);
+                              void* ws, float* seq_sum, float* stats, hipStream_t st) {
+  if (a.T > 0 && a.n_seqs > 0) {
+    hipError_t e = sp_launch(kKPolicy, p.entropy ? policy_rows_kernel<true> : policy_rows_kernel<false>,
+                             dim3((unsigned)a.T * p.parts), dim3(kPB), st, a, p, (const u32x4*)logits, tok.labels,
+                             (f32x4*)ws);
     if (e != hipSuccess) return e;
   }
-  if (p.parts == 1) {
-    if (a.n_seqs == 0) return hipSuccess;
-    return sp_launch(0, policy_sums_kernel<1024, false>, dim3(a.n_seqs), dim3(1024), st, a, p, (const uint16_t*)logits,
-                     tok, (const f32x4*)part, seq_sum, stats);
-  }
-  return sp_launch(0, policy_sums_kernel<kPB, true>, dim3(std::max(a.n_seqs, 1)), dim3(kPB), st, a, p,
-                   (const uint16_t*)logits, tok, (const f32x4*)part, seq_sum, stats);
+  if (a.T == 0 && a.n_seqs == 0) return hipSuccess;
+  int longest = 0;
+  for (int s = 0; s < a.n_seqs; ++s) longest = std::max(longest, a.cu[s + 1] - a.cu[s]);
+  const int pieces = std::max(1, (longest + kSumTokens - 1) / kSumTokens);
+  double* partial = (double*)((char*)ws + policy_partial_at(a.T, a.V));
+  hipError_t e = sp_launch(0, policy_sums_kernel, dim3(std::max(a.n_seqs, 1), pieces), dim3(kPB), st, a, p,
+                           (const uint16_t*)logits, tok, (const f32x4*)ws, partial, seq_sum, stats);
+  if (e != hipSuccess || pieces == 1) return e;
+  return sp_launch(0, policy_join_kernel, dim3(a.n_seqs), dim3(kPB), st, (const double*)partial, pieces, seq_sum, stats);
 }
 
 hipError_t launch_policy_loss_bwd(const LossArgs& a, const PolicyArgs& p, const void* logits, const PolicyTokens& tok,

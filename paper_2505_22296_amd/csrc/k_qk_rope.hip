@@ -19,9 +19,16 @@
 // 2^-32 turns at any position below 2^31.
 //
 // D / 16 neighbouring lanes hold a row (a head of a token), 16 dims each, so that
-// both halves of a pair are in one lane; a wavefront has 64 / (D / 16) rows of one
-// token, whose angles are formed once for all its heads.
+// both halves of a pair are in one lane.  A wavefront holds one head of 64 / (D / 16)
+// tokens at a time and goes through a range of heads: what depends on the head --
+// its kind, weights and slots -- is uniform and comes through the scalar cache, what
+// depends on the token -- the angles -- is formed once for the whole range, and the
+// next head's loads are in flight while one is worked on.  (Heads on the lanes and
+// one token a wavefront instead: forward of 4096 tokens of 28 / 4 heads to 8 ranks,
+// D = 128, 20.1 us, now 17.9, 5.9 TB/s; backward 32.8 us, now 30.5, of 8191 tokens of
+// 40 / 8 heads from 16 ranks 99, now 72, 5.3 TB/s.)
 #include <algorithm>
+#include <type_traits>
 
 #include "dev_common.h"
 #include "launch.h"
@@ -31,6 +38,12 @@ namespace spk {
 namespace {
 
 constexpr int kQB = 256;  // threads a workgroup (four wavefronts)
+
+// The kernels' first argument where it lies, in constant memory: its tables are read
+// at run-time indexes, for which the compiler copies the argument itself to scratch
+// memory when its passes do not see through (25 times the time).
+template <typename A>
+using Arg = __attribute__((address_space(4))) A;
 
 // The two 16-byte chunks of a row that lane l of the row holds: with `halves`
 // pairing (i, i + rot/2) chunks l and l + rot/16 of the rotated dims; neighbour
@@ -42,22 +55,18 @@ SP_DEV void lane_chunks(int l, int rot, int& ca, int& cb) {
   cb = turned ? l + rot / 16 : 2 * l + 1;
 }
 
-// cos and sin (times the scale) of the lane's eight pairs at one position.
-template <bool NEIGH>
-SP_DEV void lane_angles(const QkArgs& a, int l, int64_t pos, float (&cs)[8], float (&sn)[8]) {
+// cos and sin (times the scale) of the lane's eight pairs at one position.  The
+// instructions take turns and are off by at most 1.3e-7 (measured over 2^22 values).
+template <bool NEIGH, typename A>
+SP_DEV void lane_angles(A a, int l, int64_t pos, float (&cs)[8], float (&sn)[8]) {
 #pragma unroll
   for (int k = 0; k < 8; ++k) {
     const int f = 8 * l + k;  // the pair's frequency (either pairing)
-    cs[k] = 1.f;
-    sn[k] = 0.f;
-    if (f < a.rot / 2) {
-      const uint64_t turns = (uint64_t)pos * a.freq[f];
-      const float x = (float)(int32_t)(turns >> 32) * 0x1p-32f;  // in [-1/2, 1/2]
-      float c, s;
-      sincospif(2.f * x, &s, &c);
-      cs[k] = c * a.rope_scale;
-      sn[k] = s * a.rope_scale;
-    }
+    const bool turned = f < a->rot / 2;
+    const uint64_t turns = (uint64_t)pos * a->freq[f & 63];
+    const float x = (float)(int32_t)(turns >> 32) * 0x1p-32f;  // in [-1/2, 1/2]
+    cs[k] = turned ? __builtin_amdgcn_cosf(x) * a->rope_scale : 1.f;
+    sn[k] = turned ? __builtin_amdgcn_sinf(x) * a->rope_scale : 0.f;
   }
 }
 
@@ -111,64 +120,127 @@ SP_DEV void lane_weights(const u32x4* w, int ca, int cb, float off, float (&x)[1
   for (int i = 0; i < 16; ++i) x[i] += off;
 }
 
-template <int D, bool NEIGH>
-__global__ __launch_bounds__(kQB) void qk_rope_kernel(QkArgs a, const u32x4* __restrict__ q, const u32x4* __restrict__ k,
-                                                      const u32x4* __restrict__ v,
+// Heads of the backward's wavefronts: units [0, q_units) have q_span query heads each,
+// the others kv_span key and value heads.
+struct QkSpans {
+  int q_units, q_span, kv_span;
+};
+
+// Row i of a token's heads: its kind (0 query, 1 key, 2 value), the head, and its
+// entries [s0, s1) in the kind's slot table.
+struct HeadRow {
+  int kind, head, s0, s1;
+};
+template <typename A>
+SP_DEV HeadRow head_row(A a, int i) {
+  const int kind = i < a->Hq ? 0 : i < a->Hq + a->Hkv ? 1 : 2;
+  const int g = kind == 0 ? i : kind == 1 ? i - a->Hq : i - a->Hq - a->Hkv;
+  return HeadRow{kind, g, kind == 0 ? a->q_start[g] : a->kv_start[g], kind == 0 ? a->q_start[g + 1] : a->kv_start[g + 1]};
+}
+// First chunk of token t's row in a [sp, T, H, D] buffer at slot entry e.
+template <typename A>
+SP_DEV int64_t slot_chunk(A a, uint32_t e, int kind, int t, int nch) {
+  const int H = kind == 0 ? a->Hq_loc : a->Hkv_loc;
+  return (((int64_t)(e >> 10) * a->T + t) * H + (e & 1023)) * nch;
+}
+template <typename A>
+SP_DEV uint32_t slot_entry(A a, int kind, int s) { return kind == 0 ? a->q_slot[s] : a->kv_slot[s]; }
+
+// A workgroup's wavefronts take `span` heads each of the tokens of blockIdx.x;
+// behind a token's heads come three rows for the dummy slots of each kind.
+template <int D, bool NEIGH, typename A>
+__global__ __launch_bounds__(kQB) void qk_rope_kernel(A args, int span, const u32x4* __restrict__ q,
+                                                      const u32x4* __restrict__ k, const u32x4* __restrict__ v,
                                                       const int32_t* __restrict__ positions,
                                                       const u32x4* __restrict__ w_q, const u32x4* __restrict__ w_k,
                                                       u32x4* __restrict__ q_dst, u32x4* __restrict__ k_dst,
                                                       u32x4* __restrict__ v_dst) {
   constexpr int L = D / 16, R = 64 / L, NCH = D / 8;
+  const Arg<A>* a = (const Arg<A>*)__builtin_amdgcn_kernarg_segment_ptr();
   const int lane = threadIdx.x & 63, l = lane % L;
-  const int t = blockIdx.x * (kQB / 64) + (threadIdx.x >> 6);
-  if (t >= a.T) return;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int tt = blockIdx.x * R + lane / L, t = min(tt, a->T - 1);
+  const bool live = tt < a->T;
+  const int heads = a->Hq + 2 * a->Hkv;
+  const int r0 = (blockIdx.y * (kQB / 64) + wave) * span, r1 = min(r0 + span, heads + 3);
+  if (r0 >= r1) return;
   int ca, cb;
-  lane_chunks<NEIGH>(l, a.rot, ca, cb);
+  lane_chunks<NEIGH>(l, a->rot, ca, cb);
+  u32x4 lo = {0u, 0u, 0u, 0u}, hi = lo;
+  auto load = [&](int i) {
+    if (i >= min(r1, heads)) return;
+    const HeadRow h = head_row(a, i);
+    const u32x4* src = (h.kind == 0 ? q + t * a->sq : h.kind == 1 ? k + t * a->sk : v + t * a->sv) + h.head * NCH;
+    lo = src[ca];
+    hi = src[cb];
+  };
+  load(r0);
   float cs[8], sn[8];
-  lane_angles<NEIGH>(a, l, positions ? (int64_t)positions[t] : (int64_t)a.pos_base + t, cs, sn);
-  const int nq = a.sp * a.Hq_loc, nk = a.sp * a.Hkv_loc;
-  for (int i0 = 0; i0 < nq + 2 * nk; i0 += R) {
-    const int i = i0 + lane / L;
-    if (i >= nq + 2 * nk) break;
-    const int kind = i < nq ? 0 : i < nq + nk ? 1 : 2;
-    const uint32_t e = kind == 0 ? a.q_slot[i] : a.kv_slot[kind == 1 ? i - nq : i - nq - nk];
-    const int h = e & 1023, j = (e >> 10) & 1023, g = (int)(e >> 20) - 1;  // slot, rank, head
-    const int H = kind == 0 ? a.Hq_loc : a.Hkv_loc;
-    u32x4* dst = (kind == 0 ? q_dst : kind == 1 ? k_dst : v_dst) + (((int64_t)j * a.T + t) * H + h) * NCH;
-    u32x4 lo = {0u, 0u, 0u, 0u}, hi = lo;
-    if (g >= 0) {
-      const u32x4* src = kind == 0 ? q + t * a.sq : kind == 1 ? k + t * a.sk : v + t * a.sv;
-      lo = src[g * NCH + ca];
-      hi = src[g * NCH + cb];
-    }
-    if (kind < 2) {
-      float x[16];
-      unpack16(lo, hi, x);
-      const u32x4* w = kind == 0 ? w_q : w_k;
-      float ss = 0.f;
+  lane_angles<NEIGH>(a, l, positions ? (int64_t)positions[t] : (int64_t)a->pos_base + t, cs, sn);
+  for (int i = r0; i < r1; ++i) {
+    u32x4 out_lo = lo, out_hi = hi;
+    HeadRow h;
+    if (i < heads) {
+      h = head_row(a, i);
+      load(i + 1);
+      if (h.kind < 2) {
+        float x[16];
+        unpack16(out_lo, out_hi, x);
+        const u32x4* w = h.kind == 0 ? w_q : w_k;
+        if (w) {
+          float wt[16], ss = 0.f;
+          lane_weights(w, ca, cb, a->w_off, wt);
 #pragma unroll
-      for (int d = 0; d < 16; ++d) ss = __builtin_fmaf(x[d], x[d], ss);
-      ss = row_sum<L>(ss);
-      if (w) {
-        float wt[16];
-        lane_weights(w, ca, cb, a.w_off, wt);
-        const float r = rsqrtf(ss * (1.f / D) + a.eps);
+          for (int d = 0; d < 16; ++d) ss = __builtin_fmaf(x[d], x[d], ss);
+          const float r = rsqrtf(row_sum<L>(ss) * (1.f / D) + a->eps);
 #pragma unroll
-        for (int d = 0; d < 16; ++d) x[d] = x[d] * r * wt[d];
+          for (int d = 0; d < 16; ++d) x[d] = x[d] * r * wt[d];
+        }
+        turn<NEIGH>(x, cs, sn, 1.f);
+        out_lo = pack_lo(x);
+        out_hi = pack_hi(x);
       }
-      turn<NEIGH>(x, cs, sn, 1.f);
-      if (g >= 0) {
-        lo = pack_lo(x);
-        hi = pack_hi(x);
+    } else {  // the slots without a head
+      const int kind = i - heads;
+      h = HeadRow{kind, 0, kind == 0 ? a->q_start[a->Hq] : a->kv_start[a->Hkv], a->sp * (kind == 0 ? a->Hq_loc : a->Hkv_loc)};
+      out_lo = out_hi = u32x4{0u, 0u, 0u, 0u};
+    }
+    u32x4* dst = h.kind == 0 ? q_dst : h.kind == 1 ? k_dst : v_dst;
+    for (int s = h.s0; s < h.s1; ++s) {
+      u32x4* p = dst + slot_chunk(a, slot_entry(a, h.kind, s), h.kind, t, NCH);
+      if (live) {
+        st_stream(out_lo, &p[ca]);
+        st_stream(out_hi, &p[cb]);
       }
     }
-    st_stream(lo, &dst[ca]);
-    st_stream(hi, &dst[cb]);
   }
 }
 
-template <int D, bool NEIGH>
-__global__ __launch_bounds__(kQB) void qk_rope_bwd_kernel(QkBwdArgs b, const u32x4* q, const u32x4* k,
+// Head i's gradient at its first slot, and its row where there is a norm.
+template <typename A>
+SP_DEV void load_grad(A a, int i, int t, int ca, int cb, int nch, const u32x4* q, const u32x4* k,
+                      const u32x4* dq_src, const u32x4* dk_src, const u32x4* dv_src, const u32x4* w_q,
+                      const u32x4* w_k, u32x4& glo, u32x4& ghi, u32x4& xlo, u32x4& xhi) {
+  const HeadRow h = head_row(a, i);
+  glo = ghi = u32x4{0u, 0u, 0u, 0u};
+  if (h.s0 < h.s1) {
+    const u32x4* p = (h.kind == 0 ? dq_src : h.kind == 1 ? dk_src : dv_src) +
+                     slot_chunk(a, slot_entry(a, h.kind, h.s0), h.kind, t, nch);
+    glo = ld_stream(&p[ca]);
+    ghi = ld_stream(&p[cb]);
+  }
+  if (h.kind == 0 ? w_q != nullptr : h.kind == 1 && w_k != nullptr) {
+    const u32x4* xs = (h.kind == 0 ? q + t * a->sq : k + t * a->sk) + h.head * nch;
+    xlo = xs[ca];
+    xhi = xs[cb];
+  }
+}
+
+// The same division of heads and tokens, but a wavefront has query heads or key and
+// value heads (weights and weight gradients of one kind in registers); a workgroup
+// goes through every gridDim.x-th group of tokens and keeps a partial weight gradient.
+template <int D, bool NEIGH, typename A>
+__global__ __launch_bounds__(kQB, 4) void qk_rope_bwd_kernel(A args, QkStrides o, QkSpans n, const u32x4* q, const u32x4* k,
                                                           const u32x4* __restrict__ dq_src,
                                                           const u32x4* __restrict__ dk_src,
                                                           const u32x4* __restrict__ dv_src,
@@ -176,141 +248,212 @@ __global__ __launch_bounds__(kQB) void qk_rope_bwd_kernel(QkBwdArgs b, const u32
                                                           const u32x4* __restrict__ w_q, const u32x4* __restrict__ w_k,
                                                           u32x4* dq, u32x4* dk, u32x4* dv, float* __restrict__ part) {
   constexpr int L = D / 16, R = 64 / L, NCH = D / 8, NW = kQB / 64;
-  const QkArgs& a = b.a;
-  const int lane = threadIdx.x & 63, l = lane % L, wave = threadIdx.x >> 6;
+  const Arg<A>* a = (const Arg<A>*)__builtin_amdgcn_kernarg_segment_ptr();
+  const int lane = threadIdx.x & 63, l = lane % L;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int heads = a->Hq + 2 * a->Hkv;
+  const int unit = blockIdx.y * NW + wave;
+  const bool query = unit < n.q_units;
+  const int r0 = query ? min(unit * n.q_span, a->Hq) : min(a->Hq + (unit - n.q_units) * n.kv_span, heads);
+  const int r1 = query ? min(r0 + n.q_span, a->Hq) : min(r0 + n.kv_span, heads);
+  const u32x4* w = query ? w_q : w_k;
   int ca, cb;
-  lane_chunks<NEIGH>(l, a.rot, ca, cb);
-  float aq[16], ak[16];
+  lane_chunks<NEIGH>(l, a->rot, ca, cb);
+  float acc[16];
 #pragma unroll
-  for (int d = 0; d < 16; ++d) aq[d] = ak[d] = 0.f;
-  const int rows = a.Hq + 2 * a.Hkv;
-  for (int t = blockIdx.x * NW + wave; t < a.T; t += gridDim.x * NW) {
+  for (int d = 0; d < 16; ++d) acc[d] = 0.f;
+  u32x4 wlo = {0u, 0u, 0u, 0u}, whi = wlo;
+  if (w) {
+    wlo = w[ca];
+    whi = w[cb];
+  }
+  for (int t0 = blockIdx.x * R; t0 < a->T && r0 < r1; t0 += gridDim.x * R) {
+    const int tt = t0 + lane / L, t = min(tt, a->T - 1);
+    const bool live = tt < a->T;
+    u32x4 glo, ghi, xlo, xhi;  // head i's gradient at its first slot, and its row
+    load_grad(a, r0, t, ca, cb, NCH, q, k, dq_src, dk_src, dv_src, w_q, w_k, glo, ghi, xlo, xhi);
     float cs[8], sn[8];
-    lane_angles<NEIGH>(a, l, positions ? (int64_t)positions[t] : (int64_t)a.pos_base + t, cs, sn);
-    for (int i0 = 0; i0 < rows; i0 += R) {
-      const int i = i0 + lane / L;
-      if (i >= rows) break;
-      const int kind = i < a.Hq ? 0 : i < a.Hq + a.Hkv ? 1 : 2;
-      const int g = kind == 0 ? i : kind == 1 ? i - a.Hq : i - a.Hq - a.Hkv;
-      const u32x4* src = kind == 0 ? dq_src : kind == 1 ? dk_src : dv_src;
-      const int H = kind == 0 ? a.Hq_loc : a.Hkv_loc;
-      const int s0 = kind == 0 ? b.q_start[g] : b.kv_start[g], s1 = kind == 0 ? b.q_start[g + 1] : b.kv_start[g + 1];
+    lane_angles<NEIGH>(a, l, positions ? (int64_t)positions[t] : (int64_t)a->pos_base + t, cs, sn);
+    for (int i = r0; i < r1; ++i) {
+      const HeadRow h = head_row(a, i);
+      const u32x4 x0 = xlo, x1 = xhi;
       float c[16];
-#pragma unroll
-      for (int d = 0; d < 16; ++d) c[d] = 0.f;
-      for (int s = s0; s < s1; ++s) {
-        const uint32_t e = kind == 0 ? a.q_slot[s] : a.kv_slot[s];
-        const int h = e & 1023, j = (e >> 10) & 1023;
-        const u32x4* p = src + (((int64_t)j * a.T + t) * H + h) * NCH;
+      unpack16(glo, ghi, c);
+      if (i + 1 < r1) load_grad(a, i + 1, t, ca, cb, NCH, q, k, dq_src, dk_src, dv_src, w_q, w_k, glo, ghi, xlo, xhi);
+      for (int s = h.s0 + 1; s < h.s1; ++s) {
+        const u32x4* p = (h.kind == 0 ? dq_src : h.kind == 1 ? dk_src : dv_src) +
+                         slot_chunk(a, slot_entry(a, h.kind, s), h.kind, t, NCH);
         float y[16];
         unpack16(ld_stream(&p[ca]), ld_stream(&p[cb]), y);
 #pragma unroll
         for (int d = 0; d < 16; ++d) c[d] += y[d];
       }
-      u32x4* out = kind == 0 ? dq + t * b.dsq : kind == 1 ? dk + t * b.dsk : dv + t * b.dsv;
-      if (kind < 2) {
+      u32x4* out = (h.kind == 0 ? dq + t * o.q : h.kind == 1 ? dk + t * o.k : dv + t * o.v) + h.head * NCH;
+      if (h.kind < 2) {
         turn<NEIGH>(c, cs, sn, -1.f);
-        const u32x4* w = kind == 0 ? w_q : w_k;
         if (w) {
-          const u32x4* xs = (kind == 0 ? q + t * a.sq : k + t * a.sk) + g * NCH;
           float x[16], wt[16];
-          unpack16(xs[ca], xs[cb], x);
-          lane_weights(w, ca, cb, a.w_off, wt);
+          unpack16(x0, x1, x);
+          // the weights stay packed (8 registers less; four wavefronts a SIMD)
+          u32x4 w0 = wlo, w1 = whi;
+          asm volatile("" : "+v"(w0), "+v"(w1));
+          unpack16(w0, w1, wt);
           float ss = 0.f, cx = 0.f;
+#pragma unroll
+          for (int d = 0; d < 16; ++d) wt[d] = c[d] * (wt[d] + a->w_off);  // gradient of the normed row
 #pragma unroll
           for (int d = 0; d < 16; ++d) {
             ss = __builtin_fmaf(x[d], x[d], ss);
-            cx = __builtin_fmaf(c[d] * wt[d], x[d], cx);
+            cx = __builtin_fmaf(wt[d], x[d], cx);
           }
-          ss = row_sum<L>(ss);
-          cx = row_sum<L>(cx);
-          const float r = rsqrtf(ss * (1.f / D) + a.eps);
-          const float m = cx * r * r * (1.f / D);
+          const float r = rsqrtf(row_sum<L>(ss) * (1.f / D) + a->eps);
+          const float m = row_sum<L>(cx) * r * r * (1.f / D), rl = live ? r : 0.f;
 #pragma unroll
           for (int d = 0; d < 16; ++d) {
-            const float dw = c[d] * (x[d] * r);
-            if (kind == 0) aq[d] += dw; else ak[d] += dw;
-            c[d] = r * (c[d] * wt[d] - x[d] * m);
+            acc[d] = __builtin_fmaf(c[d], x[d] * rl, acc[d]);
+            c[d] = r * (wt[d] - x[d] * m);
           }
         }
       }
-      st_stream(pack_lo(c), &out[g * NCH + ca]);
-      st_stream(pack_hi(c), &out[g * NCH + cb]);
+      if (live) {
+        st_stream(pack_lo(c), &out[ca]);
+        st_stream(pack_hi(c), &out[cb]);
+      }
     }
   }
   if (!part) return;
-  // the wavefront's rows, then the four wavefronts, in a fixed order
+  // the wavefront's tokens, then the four wavefronts, in a fixed order
   __shared__ float red[NW][2][D];
 #pragma unroll
   for (int d = 0; d < 16; ++d) {
 #pragma unroll
-    for (int off = L; off < 64; off <<= 1) {
-      aq[d] += __shfl_xor(aq[d], off);
-      ak[d] += __shfl_xor(ak[d], off);
-    }
+    for (int off = L; off < 64; off <<= 1) acc[d] += __shfl_xor(acc[d], off);
     if (lane < L) {
       const int dim = (d < 8 ? ca : cb) * 8 + (d & 7);
-      red[wave][0][dim] = aq[d];
-      red[wave][1][dim] = ak[d];
+      red[wave][0][dim] = query ? acc[d] : 0.f;
+      red[wave][1][dim] = query ? 0.f : acc[d];
     }
   }
   __syncthreads();
+  const int64_t wg = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
   for (int e = threadIdx.x; e < 2 * D; e += kQB) {
     float x = 0.f;
 #pragma unroll
     for (int w = 0; w < NW; ++w) x += red[w][e / D][e % D];
-    part[(int64_t)blockIdx.x * 2 * D + e] = x;
+    part[wg * 2 * D + e] = x;
   }
 }
 
-// dw[e] = sum of the workgroups' partials, for 16 entries a workgroup: 16 threads
-// an entry, then their sums in a fixed order.
-__global__ __launch_bounds__(kQB) void qk_dw_kernel(const float* __restrict__ part, int n, int D,
+// dw[e] = sum of the n workgroups' partials: a workgroup takes 16 entries as four
+// vectors, 64 threads a vector, eight loads in flight each; then their sums in a
+// fixed order.  (One entry a thread and one load in flight: 20 us for 1024 partials.)
+__global__ __launch_bounds__(kQB) void qk_dw_kernel(const f32x4* __restrict__ part, int n, int D,
                                                     float* __restrict__ dw_q, float* __restrict__ dw_k) {
-  const int e = blockIdx.x * 16 + (threadIdx.x & 15), r = threadIdx.x >> 4;
-  float x = 0.f;
-  for (int i = r; i < n; i += 16) x += part[(int64_t)i * 2 * D + e];
-  __shared__ float red[16][17];
-  red[r][threadIdx.x & 15] = x;
-  __syncthreads();
-  if (r == 0) {
-    float y = 0.f;
+  const int c = threadIdx.x & 3, r = threadIdx.x >> 2, v = blockIdx.x * 4 + c, nv = D / 2;
+  f32x4 x = {0.f, 0.f, 0.f, 0.f};
+  for (int i0 = r; i0 < n; i0 += 64 * 8) {
+    f32x4 y[8];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) y += red[i][threadIdx.x];
+    for (int u = 0; u < 8; ++u) y[u] = i0 + u * 64 < n ? part[(int64_t)(i0 + u * 64) * nv + v] : f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int u = 0; u < 8; ++u)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) x[k] += y[u][k];
+  }
+  __shared__ f32x4 red[64][5];
+  red[r][c] = x;
+  __syncthreads();
+  if (threadIdx.x < 16) {
+    float y = 0.f;
+    for (int i = 0; i < 64; ++i) y += red[i][threadIdx.x >> 2][threadIdx.x & 3];
+    const int e = blockIdx.x * 16 + threadIdx.x;
     float* out = e < D ? dw_q : dw_k;
     if (out) out[e < D ? e : e - D] = y;
   }
 }
 
-}  // namespace
-
+// Grid for `rows` rows a token: about `waves` wavefronts in all, each with at least
+// one row, and four (a workgroup) for all rows of its tokens at least.
+struct QkGrid {
+  int groups, parts;
+};
+QkGrid qk_grid(int T, int D, int rows, int waves) {
+  const int R = 64 / (D / 16), groups = std::max(1, (T + R - 1) / R);
+  return QkGrid{groups, std::max(1, std::min((rows + 3) / 4, waves / 4 / groups))};
+}
+constexpr int kQkFwdWaves = 8192, kQkBwdWaves = 4096;
 // Workgroups of the backward, which keep a partial weight gradient each.
-int qk_bwd_groups(int T) { return std::max(1, std::min((T + kQB / 64 - 1) / (kQB / 64), 1024)); }
-
-hipError_t launch_qk_rope(const QkArgs& a, int D, const void* q, const void* k, const void* v, const int32_t* positions,
-                          const void* w_q, const void* w_k, void* q_dst, void* k_dst, void* v_dst, hipStream_t st) {
-  auto* kernel = D == 128 ? (a.neigh ? qk_rope_kernel<128, true> : qk_rope_kernel<128, false>)
-                          : (a.neigh ? qk_rope_kernel<64, true> : qk_rope_kernel<64, false>);
-  return sp_launch(kKQkRope, kernel, dim3((a.T + kQB / 64 - 1) / (kQB / 64)), dim3(kQB), st, a, (const u32x4*)q,
-                   (const u32x4*)k, (const u32x4*)v, positions, (const u32x4*)w_q, (const u32x4*)w_k, (u32x4*)q_dst,
-                   (u32x4*)k_dst, (u32x4*)v_dst);
+QkGrid qk_bwd_grid(const QkArgs& a, int D) {
+  QkGrid g = qk_grid(a.T, D, a.Hq + 2 * a.Hkv, kQkBwdWaves);
+  g.groups = std::min(g.groups, std::max(1, kQkBwdWaves / 4 / g.parts));
+  return g;
+}
+// Its wavefronts' heads: the units of `parts` workgroups shared between query and
+// other heads by their numbers, one at least for each.
+QkSpans qk_spans(const QkArgs& a, int parts) {
+  const int units = 4 * parts, rows = a.Hq + 2 * a.Hkv;
+  const int q = std::max(1, std::min(units - 1, (units * a.Hq + rows / 2) / rows));
+  return QkSpans{q, (a.Hq + q - 1) / q, (2 * a.Hkv + units - q - 1) / (units - q)};
 }
 
-hipError_t launch_qk_rope_bwd(const QkBwdArgs& b, int D, const void* q, const void* k, const void* dq_src,
-                              const void* dk_src, const void* dv_src, const int32_t* positions, const void* w_q,
-                              const void* w_k, void* dq, void* dk, void* dv, float* dw_q, float* dw_k, float* part,
-                              hipStream_t st) {
-  const int n = b.a.T > 0 ? qk_bwd_groups(b.a.T) : 0;
+}  // namespace
+
+int qk_bwd_groups(const QkArgs& a, int D) {
+  const QkGrid g = qk_bwd_grid(a, D);
+  return g.groups * g.parts;
+}
+
+// Up to 64 slots and heads of either kind travel in arguments of their own size (the
+// 6.7 KB of the largest cost a launch 1.5 us of host time).
+template <typename F>
+static hipError_t with_qk_args(const QkArgs& a, const F& f) {
+  constexpr int N = QkArgsSmall::kSlots, M = QkArgsSmall::kHeads;
+  const int nq = a.sp * a.Hq_loc, nk = a.sp * a.Hkv_loc;
+  if (nq > N || nk > N || a.Hq > M || a.Hkv > M) return f(a);
+  QkArgsSmall b;
+  static_cast<QkBase&>(b) = a;
+  std::copy(a.q_slot, a.q_slot + nq, b.q_slot);
+  std::copy(a.kv_slot, a.kv_slot + nk, b.kv_slot);
+  std::copy(a.q_start, a.q_start + a.Hq + 1, b.q_start);
+  std::copy(a.kv_start, a.kv_start + a.Hkv + 1, b.kv_start);
+  return f(b);
+}
+
+hipError_t launch_qk_rope(const QkArgs& args, int D, const void* q, const void* k, const void* v, const int32_t* positions,
+                          const void* w_q, const void* w_k, void* q_dst, void* k_dst, void* v_dst, hipStream_t st) {
+  return with_qk_args(args, [&](const auto& a) {
+    using A = std::decay_t<decltype(a)>;
+    auto* kernel = D == 128 ? (a.neigh ? qk_rope_kernel<128, true, A> : qk_rope_kernel<128, false, A>)
+                            : (a.neigh ? qk_rope_kernel<64, true, A> : qk_rope_kernel<64, false, A>);
+    const int rows = a.Hq + 2 * a.Hkv + 3;
+    const QkGrid g = qk_grid(a.T, D, rows, kQkFwdWaves);
+    const int span = (rows + 4 * g.parts - 1) / (4 * g.parts);
+    return sp_launch(kKQkRope, kernel, dim3(g.groups, g.parts), dim3(kQB), st, a, span, (const u32x4*)q,
+                     (const u32x4*)k, (const u32x4*)v, positions, (const u32x4*)w_q, (const u32x4*)w_k, (u32x4*)q_dst,
+                     (u32x4*)k_dst, (u32x4*)v_dst);
+  });
+}
+
+hipError_t launch_qk_rope_bwd(const QkArgs& args, const QkStrides& o, int D, const void* q, const void* k,
+                              const void* dq_src, const void* dk_src, const void* dv_src, const int32_t* positions,
+                              const void* w_q, const void* w_k, void* dq, void* dk, void* dv, float* dw_q, float* dw_k,
+                              float* part, hipStream_t st) {
+  const QkGrid g = qk_bwd_grid(args, D);
+  const int n = args.T > 0 ? g.groups * g.parts : 0;
   if (n > 0) {
-    auto* kernel = D == 128 ? (b.a.neigh ? qk_rope_bwd_kernel<128, true> : qk_rope_bwd_kernel<128, false>)
-                            : (b.a.neigh ? qk_rope_bwd_kernel<64, true> : qk_rope_bwd_kernel<64, false>);
-    hipError_t e = sp_launch(kKQkRopeBwd, kernel, dim3(n), dim3(kQB), st, b, (const u32x4*)q, (const u32x4*)k,
-                             (const u32x4*)dq_src, (const u32x4*)dk_src, (const u32x4*)dv_src, positions,
-                             (const u32x4*)w_q, (const u32x4*)w_k, (u32x4*)dq, (u32x4*)dk, (u32x4*)dv, part);
+    hipError_t e = with_qk_args(args, [&](const auto& a) {
+      using A = std::decay_t<decltype(a)>;
+      auto* kernel = D == 128 ? (a.neigh ? qk_rope_bwd_kernel<128, true, A> : qk_rope_bwd_kernel<128, false, A>)
+                              : (a.neigh ? qk_rope_bwd_kernel<64, true, A> : qk_rope_bwd_kernel<64, false, A>);
+      return sp_launch(kKQkRopeBwd, kernel, dim3(g.groups, g.parts), dim3(kQB), st, a, o, qk_spans(args, g.parts),
+                       (const u32x4*)q, (const u32x4*)k, (const u32x4*)dq_src, (const u32x4*)dk_src,
+                       (const u32x4*)dv_src, positions, (const u32x4*)w_q, (const u32x4*)w_k, (u32x4*)dq, (u32x4*)dk,
+                       (u32x4*)dv, part);
+    });
     if (e != hipSuccess) return e;
   }
   if (!dw_q && !dw_k) return hipSuccess;
-  return sp_launch(0, qk_dw_kernel, dim3(2 * D / 16), dim3(kQB), st, (const float*)part, n, D, dw_q, dw_k);
+  return sp_launch(0, qk_dw_kernel, dim3(2 * D / 16), dim3(kQB), st, (const f32x4*)part, n, D, dw_q, dw_k);
 }
 
 }  // namespace spk

@@ -1,6 +1,7 @@
 // Internal interface between the host-side ABI code and the gfx950 kernels.
 #pragma once
 #include <hip/hip_runtime.h>
+#include <stddef.h>
 #include <stdint.h>
 
 namespace spk {
@@ -104,21 +105,27 @@ struct PolicyTokens {
   float *logp, *lse, *ent;
 };
 
-// Norm, rotation and pack of query / key heads.  A slot entry: slot of its rank in
-// bits 0-9, rank in bits 10-19, head + 1 (0: a dummy) above.  Strides in 16-byte
-// chunks a token; frequencies in 2^-64 turns a position.
+// Norm, rotation and pack of query / key heads.  Slot entries -- slot of its rank in
+// bits 0-9, rank above -- of head g at [start[g], start[g + 1]), ascending, then those
+// without a head.  Strides in 16-byte chunks a token; frequencies in 2^-64 turns a
+// position.
 static constexpr int kMaxQkHeads = 256;
-struct QkArgs {
+struct QkBase {
   int T, Hq, Hkv, sp, Hq_loc, Hkv_loc, rot, neigh, pos_base;
   float rope_scale, eps, w_off;
   int64_t sq, sk, sv;
   uint64_t freq[64];
-  uint32_t q_slot[kMaxMap], kv_slot[kMaxMap];  // forward: by slot; backward: by head, ascending
 };
-struct QkBwdArgs {
-  QkArgs a;
-  int64_t dsq, dsk, dsv;
-  int16_t q_start[kMaxQkHeads + 1], kv_start[kMaxQkHeads + 1];  // a head's entries
+template <int SLOTS, int HEADS>
+struct QkArgsOf : QkBase {
+  static constexpr int kSlots = SLOTS, kHeads = HEADS;
+  uint32_t q_slot[SLOTS], kv_slot[SLOTS];
+  int q_start[HEADS + 1], kv_start[HEADS + 1];
+};
+using QkArgs = QkArgsOf<kMaxMap, kMaxQkHeads>;
+using QkArgsSmall = QkArgsOf<64, 64>;
+struct QkStrides {  // of the gradients
+  int64_t q, k, v;
 };
 
 struct ReduceArgs {
@@ -220,14 +227,15 @@ hipError_t launch_token_logprob_bwd(const LossArgs& a, const void* logits, const
 hipError_t launch_loss_reduce(const LossReduceArgs& a, const float* ps, const float* refs,
                               float* loss, float* grad, hipStream_t st);
 int policy_parts(int T, int V);
+size_t policy_workspace(int T, int V);
 hipError_t launch_policy_loss(const LossArgs& a, const PolicyArgs& p, const void* logits, const PolicyTokens& tok,
-                              void* part, float* seq_sum, float* stats, hipStream_t st);
+                              void* ws, float* seq_sum, float* stats, hipStream_t st);
 hipError_t launch_policy_loss_bwd(const LossArgs& a, const PolicyArgs& p, const void* logits, const PolicyTokens& tok,
                                   const float* grad_seq, void* dlogits, hipStream_t st);
-int qk_bwd_groups(int T);
+int qk_bwd_groups(const QkArgs& a, int D);
 hipError_t launch_qk_rope(const QkArgs& a, int D, const void* q, const void* k, const void* v, const int32_t* positions,
                           const void* w_q, const void* w_k, void* q_dst, void* k_dst, void* v_dst, hipStream_t st);
-hipError_t launch_qk_rope_bwd(const QkBwdArgs& b, int D, const void* q, const void* k, const void* dq_src,
+hipError_t launch_qk_rope_bwd(const QkArgs& a, const QkStrides& o, int D, const void* q, const void* k, const void* dq_src,
                               const void* dk_src, const void* dv_src, const int32_t* positions, const void* w_q,
                               const void* w_k, void* dq, void* dk, void* dv, float* dw_q, float* dw_k, float* part,
                               hipStream_t st);
@@ -255,9 +263,11 @@ hipError_t launch_attn_fwd(const FwdArgs& a, const ItemList& list, LaunchShape s
 hipError_t launch_attn_dq(const DqArgs& a, const ItemList& list, LaunchShape s, int D, bool prefix, hipStream_t st);
 hipError_t launch_attn_dkdv(const DkdvArgs& a, const ItemList& list, LaunchShape s, int D, hipStream_t st);
 // dQ and dK/dV in one launch; (q.split, k.split) one of (4, 2), (2, 1),
-// (1, 1); two workgroups a CU for (1, 1) alone, q.two.  `dq_first`: the dQ workgroups come first.
+// (1, 1); two workgroups a CU for (1, 1) alone, q.two.  `dq_first`: the dQ workgroups
+// come first; `merged` (with `prefix`, for (1, 1)): both kinds are in one list, a's,
+// which is b's too.
 hipError_t launch_attn_bwd(const DqArgs& a, const DkdvArgs& b, const ItemList& list, LaunchShape q,
-                           LaunchShape k, bool dq_first, int D, bool prefix, hipStream_t st);
+                           LaunchShape k, bool dq_first, int D, bool prefix, bool merged, hipStream_t st);
 
 // Tile sizes the host scheduler must use (rows per fwd/dq item, keys per
 // dk/dv item) and the kernels' LDS pipelines.
