@@ -162,7 +162,9 @@ enum { SP_OP_FWD = 0, SP_OP_BWD = 1, SP_OP_RING_STEP = 2 };
  * its keys (else SP_ERR_INVALID_ARG).  A prefix without rows is one whose keys alone
  * are there.  The outputs and gradients are those of the unpacked sequences
  * [prompt, answer] with the prompt's rows counted once: dk and dv of its keys sum
- * over its own rows and every answer's.  Supported by sp_attn_fwd,
+ * over its own rows and every answer's.  A forward of few rows -- a token an answer
+ * against a long prompt -- cuts the keys into parts (sp_attn_plan; not in
+ * sp_attn_fwd_static, whose bits then differ by the roundings of the merge).  Supported by sp_attn_fwd,
  * sp_attn_fwd_static, sp_attn_bwd, sp_attn_workspace_size, sp_attn_schedule and
  * sp_attn_plan; sp_ring_step and SP_OP_RING_STEP return SP_ERR_UNSUPPORTED, and
  * SP_DESC_SINGLE_SEQUENCE beside it SP_ERR_INVALID_ARG.
@@ -414,8 +416,10 @@ sp_status sp_attn_schedule(const sp_attn_desc* desc, int32_t op, int32_t* items,
  * dimension 64); rows: the items of SP_OP_FWD / SP_OP_RING_STEP (init = 1), or
  * dQ's, keys: dK/dV's; one launch: dQ and dK/dV run in one launch, dQ first:
  * its workgroups are the first ones there (two launches of the same splits
- * where dk or dv is the k or v buffer).  The last four are 0 for the forward
- * operations.
+ * where dk or dv is the k or v buffer).  With SP_DESC_SHARED_PREFIX one launch of
+ * unsplit items has both kinds in one list, longest first.  The last four are 0 for
+ * the forward operations, but for the key split of a shared-prefix forward of few
+ * rows: the parts its keys are cut into, whose results a second kernel merges.
  */
 #define SP_PLAN_INTS 6
 sp_status sp_attn_plan(const sp_attn_desc* desc, int32_t op, int32_t* plan);

@@ -648,6 +648,14 @@ Costs schedule_row_items(const sp_attn_desc* d, const Problem& p, const std::vec
   return p.prefix.empty() ? schedule_rows(d, p, BM, BN, include_empty, out, n_front)
                           : schedule_tiles(d, p, tiles, BN, out, n_front, items);
 }
+// The model's time of a shared-prefix forward without parts.
+double whole_us(const sp_attn_desc* d, const Problem& p) {
+  std::vector<int32_t> v;
+  std::vector<Item> rows;
+  double us = 0;
+  choose_shape(schedule_tiles(d, p, row_tiles(d, p), spk::kFwdBN, v, 0, rows), kSplitFwd, p.D, us);
+  return us;
+}
 // Ints of the records under any split.
 size_t record_room(size_t n_tiles) { return n_tiles * 4 * (size_t)spk::record_ints(kSlots / 4); }
 
@@ -690,6 +698,126 @@ std::vector<int32_t> merged_items(const std::vector<Item>& rows, const std::vect
   }
   std::vector<int32_t> out;
   sort_items(all, out, n_front, false);
+  return out;
+}
+
+// A shared-prefix forward of few rows: tiles of two slots, whose keys are cut into
+// `parts`.  Taken where the model sees a fifth less time in it than in whole walks: a
+// workgroup of a part takes kStartUs and its stages of four key tiles, kFewStageUs
+// each, and the merge kFewJoinUs.  (16 answers of one row to 32768 keys, 7 heads:
+// 313 -> 36 us; one answer, 4 heads, 331 -> 30.)
+constexpr double kFewStageUs = 1.6, kFewJoinUs = 8;
+constexpr int kFewSlots = 2, kFewSplit = kSlots / kFewSlots;
+constexpr int64_t kFewBytes = int64_t(64) << 20;  // of partial results, at most
+struct FewTile {
+  int row0, row1, heads;  // rows of both slots, query heads a slot
+  int prefix, own0, own1;  // and the keys that some row sees
+  int head, kv;
+};
+struct FewPlan {
+  int parts = 0;  // 0: not taken
+  std::vector<FewTile> tiles;
+  std::vector<int32_t> windows;  // own keys [begin, end) of every row
+};
+int few_tile_steps(const Problem& p, const FewTile& t, int BN) {
+  auto steps = [&](int a, int b) { return b > a ? (b - (a & ~7) + BN - 1) / BN : 0; };
+  return (t.prefix >= 0 ? steps(p.segs[t.prefix].ka, p.segs[t.prefix].kb) : 0) + steps(t.own0, t.own1);
+}
+// `whole_us`: the model's time of the launch without parts.
+FewPlan few_plan(const sp_attn_desc* d, const Problem& p, double whole_us) {
+  FewPlan f;
+  // (a tile holds 64 rows of a head, or fewer: more rows leave no CUs for parts)
+  if (p.prefix.empty() || p.n_real == 0 || whole_us < 2 * (kStartUs + kFewJoinUs) ||
+      (int64_t)d->T_q * p.n_real > (int64_t)kCus / 2 * kFewSlots * kSlotRows ||
+      (int64_t)2 * d->T_q * d->H_loc * (p.D + 1) * 4 > kFewBytes)
+    return f;
+  std::vector<int> prefix(d->T_q, -1);
+  f.windows.assign((size_t)2 * d->T_q, 0);
+  for (size_t s = 0; s < p.segs.size(); ++s) {
+    const Seg& g = p.segs[s];
+    for (int i = g.qa; i < g.qb; ++i) {
+      prefix[i] = p.prefix[s];
+      const int k1 = d->causal ? (int)std::min<int64_t>(g.kb, (int64_t)i + g.delta + 1) : g.kb;
+      f.windows[2 * i] = g.ka;
+      f.windows[2 * i + 1] = std::max(g.ka, k1);
+    }
+  }
+  int longest = 0;
+  const int BN = spk::fwd_tile_keys(p.D, kFewSplit);
+  for (int kv = 0; kv < d->Hkv_loc; ++kv) {
+    const int n = p.kv_hi[kv] - p.kv_lo[kv], blocks = (n + kSlotRows - 1) / kSlotRows;
+    for (int b = 0; b < blocks; ++b) {
+      const int h0 = p.kv_lo[kv] + n * b / blocks, heads = p.kv_lo[kv] + n * (b + 1) / blocks - h0;
+      const int rows = kFewSlots * (kSlotRows / heads);
+      for (int i = 0; i < d->T_q;) {
+        int e = i + 1;
+        while (e < d->T_q && e < i + rows && prefix[e] == prefix[i]) ++e;
+        FewTile t{i, e, heads, prefix[i], 0, 0, h0, kv};
+        for (int r = i; r < e; ++r) {
+          const int a = f.windows[2 * r], z = f.windows[2 * r + 1];
+          if (z <= a) continue;
+          t.own0 = t.own1 > t.own0 ? std::min(t.own0, a) : a;
+          t.own1 = std::max(t.own1, z);
+        }
+        longest = std::max(longest, few_tile_steps(p, t, BN));
+        f.tiles.push_back(t);
+        i = e;
+      }
+    }
+  }
+  const int stages = (longest + kFewSplit - 1) / kFewSplit;  // of four tiles
+  const int64_t n = (int64_t)f.tiles.size(), room = kFewBytes / ((int64_t)d->T_q * d->H_loc * (p.D + 1) * 4);
+  const int parts = (int)std::min<int64_t>({(int64_t)kCus / std::max<int64_t>(n, 1), stages / 2, room, spk::kMaxParts});
+  if (parts < 2) return f;
+  const double us = kStartUs + (double)((stages + parts - 1) / parts) * kFewStageUs + kFewJoinUs;
+  if (us < 0.8 * whole_us) f.parts = parts;
+  return f;
+}
+// The items, their records and the rows' windows as one list.
+std::vector<int32_t> few_list(const sp_attn_desc* d, const Problem& p, const FewPlan& f) {
+  const int BN = spk::fwd_tile_keys(p.D, kFewSplit), ints = spk::record_ints(kFewSlots);
+  const size_t n = f.tiles.size() * f.parts, windows = n * (kItemInts + ints);
+  std::vector<int32_t> out(windows, 0);
+  for (size_t i = 0; i < n; ++i) {
+    // eight parts at a time, the tiles of each on one XCD (i % 8): they share keys
+    const size_t block = i / (kXcds * f.tiles.size()) * kXcds, width = std::min<size_t>(kXcds, f.parts - block);
+    const size_t in = i - block * f.tiles.size();
+    const FewTile& t = f.tiles[in / width];
+    const int part = (int)(block + in % width);
+    const int32_t item[kItemInts] = {(int32_t)(n * kItemInts + i * ints), part, (int32_t)windows, t.heads, 0, t.head, t.kv, 0};
+    std::copy(item, item + kItemInts, &out[i * kItemInts]);
+    int32_t* r = &out[n * kItemInts + i * ints];
+    const int all = few_tile_steps(p, t, BN);
+    const int v0 = (int)((int64_t)all * part / f.parts), v1 = (int)((int64_t)all * (part + 1) / f.parts);
+    int at = 0, n_ranges = 0, tiles = 0;
+    auto range = [&](int k0, int k1, bool prefix) {
+      if (k1 <= k0) return;
+      const int first = k0 & ~7, steps = (k1 - first + BN - 1) / BN;
+      const int a = std::max(v0, at), b = std::min(v1, at + steps);
+      if (b > a) {
+        tiles += b - a;
+        int32_t* o = r + spk::kRecordRanges + 3 * n_ranges++;
+        o[0] = tiles;
+        o[1] = first + (a - at) * BN;
+        o[2] = std::min(k1, first + (b - at) * BN);
+        if (prefix) r[1] = k0, r[2] = 1;
+      }
+      at += steps;
+    };
+    if (t.prefix >= 0) range(p.segs[t.prefix].ka, p.segs[t.prefix].kb, true);
+    range(t.own0, t.own1, false);
+    r[0] = tiles;
+    const int rows = kSlotRows / t.heads;
+    for (int s = 0; s < kFewSlots; ++s) {
+      int32_t* o = r + spk::kRecordRanges + 3 * (1 + kFewSlots) + 5 * s;
+      o[0] = std::min(t.row1, t.row0 + s * rows);
+      o[1] = std::min(t.row1, t.row0 + (s + 1) * rows);
+      o[2] = t.own0;
+      o[3] = t.own1;
+      if (o[1] <= o[0]) o[0] = o[1] = t.row0;  // (a row that exists, for addresses)
+    }
+  }
+  out.insert(out.end(), f.windows.begin(), f.windows.end());
   return out;
 }
 
@@ -736,6 +864,7 @@ int n_unread_kv(const sp_attn_desc* d, const Problem& p) {
 // Workspace layout.
 struct Layout {
   size_t items_dq = 0, items_kv = 0, neg_d = 0, lse2 = 0, part_k = 0, part_v = 0, total = 0;
+  size_t few_items = 0, few_o = 0, few_lse = 0;  // a forward of few rows
 };
 
 size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
@@ -766,6 +895,16 @@ Layout layout_for(const sp_attn_desc* d, const Problem& p, int op, size_t n_item
     }
   }
   L.total = std::max<size_t>(off, 256);
+  return L;
+}
+
+// Workspace of a shared-prefix forward of few rows.
+Layout layout_few(const sp_attn_desc* d, const Problem& p, const FewPlan& f) {
+  Layout L;
+  const size_t rows = (size_t)f.parts * d->T_q * d->H_loc;
+  L.few_o = align256(f.tiles.size() * f.parts * (kItemInts + spk::record_ints(kFewSlots)) * 4 + f.windows.size() * 4);
+  L.few_lse = L.few_o + align256(rows * p.D * 4);
+  L.total = L.few_lse + align256(rows * 4);
   return L;
 }
 
@@ -1195,6 +1334,10 @@ sp_status sp_attn_workspace_size(const sp_attn_desc* desc, int32_t op, size_t* b
   size_t a = 0, b = 0;
   item_counts(desc, p, op, a, b);
   *bytes = layout_for(desc, p, op, a, b).total;
+  if (op == SP_OP_FWD && !p.prefix.empty()) {
+    const FewPlan f = few_plan(desc, p, whole_us(desc, p));
+    if (f.parts) *bytes = layout_few(desc, p, f).total;
+  }
   return SP_OK;
 }
 
@@ -1255,6 +1398,7 @@ sp_status sp_attn_plan(const sp_attn_desc* desc, int32_t op, int32_t* plan) {
     double us;
     b.q = choose_shape(schedule_row_items(desc, p, tiles, spk::kFwdBM, spk::kFwdBN, true, v, 0, rows), kSplitFwd,
                        p.D, us);
+    b.k.split = few_plan(desc, p, us).parts;
   }
   const int32_t r[SP_PLAN_INTS] = {b.q.split, b.q.two, b.k.split, b.k.two, b.one, b.dq_first};
   std::copy(r, r + SP_PLAN_INTS, plan);
@@ -1309,6 +1453,32 @@ sp_status stream_on_current_device(hipStream_t st) {
 
 extern "C" {
 
+// A shared-prefix forward of few rows (arguments are checked).
+static sp_status fwd_few(const sp_attn_desc* d, const Problem& p, const FewPlan& few, const void* q, const void* k,
+                         const void* v, void* o, float* lse, void* ws, size_t ws_bytes, hipStream_t st) {
+  const Layout L = layout_few(d, p, few);
+  sp_status s = check_ws(L, ws, ws_bytes);
+  if (s != SP_OK) return s;
+  if ((s = refuse_capture(st)) != SP_OK) return s;
+  const std::vector<int32_t> items = few_list(d, p, few);
+  spk::FwdArgs a{};
+  spk::ItemList list{};
+  if (items.size() <= std::size(list.v)) {
+    std::copy(items.begin(), items.end(), list.v);
+  } else {
+    if ((s = upload(at(ws, L.few_items), items, st)) != SP_OK) return s;
+    a.items = (const int32_t*)at(ws, L.few_items);
+  }
+  a.q = (const uint16_t*)q; a.k = (const uint16_t*)k; a.v = (const uint16_t*)v;
+  a.o = (uint16_t*)o; a.lse = lse;
+  a.o_acc = (float*)at(ws, L.few_o); a.lse_acc = (float*)at(ws, L.few_lse);
+  a.T_q = d->T_q; a.T_k = d->T_k; a.H = d->H_loc; a.Hkv = d->Hkv_loc;
+  a.scale_log2 = d->softmax_scale * 1.4426950408889634f;
+  a.n_items = (int)(few.tiles.size() * few.parts);
+  SP_HIP(spk::launch_attn_few(a, list, p.D, few.parts, p.n_real, st));
+  return SP_OK;
+}
+
 // Forward / ring step.  `static_ws`: the work list goes to the current
 // device's static scratch instead of the caller's workspace (sp_attn_fwd_static).
 static sp_status fwd_common(const sp_attn_desc* d, const void* q, const void* k, const void* v,
@@ -1341,6 +1511,10 @@ static sp_status fwd_common(const sp_attn_desc* d, const void* q, const void* k,
   const int n_items = (int)(items.size() / kItemInts);
   double us;
   const spk::LaunchShape shape = choose_shape(cost, kSplitFwd, p.D, us);
+  if (prefix && !static_ws) {
+    const FewPlan few = few_plan(d, p, us);
+    if (few.parts) return fwd_few(d, p, few, q, k, v, o, lse, ws, ws_bytes, (hipStream_t)stream);
+  }
   if (prefix) {
     const std::vector<int32_t> records =
         place_records(d, p, tiles, shape.split, spk::fwd_tile_keys(p.D, shape.split), items, (int)items.size());

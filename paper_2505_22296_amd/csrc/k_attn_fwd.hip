@@ -45,6 +45,8 @@ namespace {
 
 constexpr int NW = kFwdWaves;         // wavefronts per workgroup
 constexpr int NT = 64 * NW;
+constexpr int kJoinThreads = 256;  // of a row's merge
+static_assert(kMaxParts <= kJoinThreads, "a part's weight a thread");
 static_assert(kFwdBM == 32 * NW, "fwd tiling");
 
 // LDS stage of the forward: for each of the KW key groups a K and a V tile
@@ -77,7 +79,20 @@ struct FwdStage {
 // TWO: at most 128 VGPRs, so that two workgroups share a CU.
 // PFX: segments share prefixes; the items name records of slots and key ranges
 // (dev_common.h), the workgroup's rows come from several segments.
-template <int D, bool MERGE, int KW, bool TWO, bool PFX>
+// FEW (with PFX, KW = 4): a call of few rows, whose items would leave most CUs idle
+// behind long walks.  An item is one workgroup with two slots and a part of their
+// keys; a slot holds 32 / g rows for each of the g query heads that share a KV head
+// (lane i: row i / g, head i % g; a token an answer then still fills a slot), of any
+// segments of one prefix, so that the own keys are a window per lane; the part's
+// normalised result goes to float32 buffers that attn_join_kernel merges.
+// (the list where it lies in the kernel arguments, for lanes' own indexes; the
+// second argument of the kernel, behind the first without a gap)
+static_assert(sizeof(FwdArgs) % alignof(ItemList) == 0, "the list follows the arguments");
+typedef const __attribute__((address_space(4))) int32_t* TablePtr;
+SP_DEV TablePtr few_rows_table(const FwdArgs& a, TablePtr list) {
+  return a.items ? (TablePtr)a.items : list;
+}
+template <int D, bool MERGE, int KW, bool TWO, bool PFX, bool FEW = false>
 __global__ __launch_bounds__(NT, TWO ? 4 : 1) void attn_fwd_kernel(FwdArgs a, ItemList list) {
   using S = FwdStage<D, KW>;
   constexpr int RW = S::RW, BN = S::BN, NST = S::NST, TPB = S::TPB;
@@ -88,11 +103,13 @@ __global__ __launch_bounds__(NT, TWO ? 4 : 1) void attn_fwd_kernel(FwdArgs a, It
 
   __shared__ u32x4 smem[S::SMEM];
 
-  int pos, sub;
-  if (!split_pos<KW>(blockIdx.x, a.n_items, pos, sub)) return;
+  int pos = blockIdx.x, sub = 0;
+  if constexpr (!FEW)
+    if (!split_pos<KW>(blockIdx.x, a.n_items, pos, sub)) return;
   int32_t it[kItemInts];
   load_item(a.items, list, 0, pos, it);
   static_assert(!PFX || !MERGE, "a ring step has no shared prefixes");
+  static_assert(!FEW || (PFX && KW == 4), "few rows");
   int q0 = it[0], q1 = it[1], k1 = it[3];
   int k0 = it[2], delta = it[4];
   const int head = it[5], kvh = it[6];
@@ -134,17 +151,26 @@ __global__ __launch_bounds__(NT, TWO ? 4 : 1) void attn_fwd_kernel(FwdArgs a, It
     has_prefix = table_at(a.items, list, record + 2) != 0;
   }
   const int wr0 = PFX ? q0 : q0 + rg * 32;  // the wavefront's first row
-  const int row = wr0 + l32;
-  const bool row_ok = row < q1;
+  const int g = FEW ? it[3] : 1;            // query heads in a slot
+  const int row = wr0 + (FEW ? l32 / g : l32);
+  const bool row_ok = FEW ? row < q1 && l32 < 32 / g * g : row < q1;
+  const int qhead = FEW ? head + l32 % g : head;
+  int own0 = 0, own1 = 0;  // FEW: the row's window of its own segment's keys
+  if constexpr (FEW) {
+    const TablePtr args = (TablePtr)__builtin_amdgcn_kernarg_segment_ptr();
+    const TablePtr win = few_rows_table(a, args + sizeof(FwdArgs) / 4) + it[2] + 2 * (row_ok ? row : q0);
+    own0 = win[0];
+    own1 = win[1];
+  }
   // last key any row of this wavefront may see (tiles past it are skipped; PFX:
   // of its own segment)
   const int wave_rows = min(32, q1 - wr0);
-  const int wave_kmax = wave_rows <= 0 ? -1 : a.causal ? min(k1, wr0 + wave_rows + delta) : k1;
+  const int wave_kmax = wave_rows <= 0 ? -1 : a.causal && !FEW ? min(k1, wr0 + wave_rows + delta) : k1;
 
   // Q^T as B operand: lane holds query row `row`, dims ks*16 + hh*8 + [0..7].
   u32x4 qf[KS];
   {
-    const uint16_t* qp = a.q + ((int64_t)(row_ok ? row : q0) * a.H + head) * D + hh * 8;
+    const uint16_t* qp = a.q + ((int64_t)(row_ok ? row : q0) * a.H + (row_ok ? qhead : head)) * D + hh * 8;
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
       qf[s] = *(const u32x4*)(qp + s * 16);
@@ -246,7 +272,8 @@ __global__ __launch_bounds__(NT, TWO ? 4 : 1) void attn_fwd_kernel(FwdArgs a, It
       int kt = kt_first + (n * KW + kg) * BN;
       // what the wavefront sees of the tile: keys [m0, m1), under the causal rule if
       // `causal`, none of them where kt >= kmax
-      int m0 = k0, m1 = k1, causal = a.causal, kmax = wave_kmax;
+      int m0 = k0, m1 = k1, causal = FEW ? 0 : a.causal, kmax = wave_kmax;
+      int own = FEW;
       if constexpr (PFX) {
         const int v = n * KW + kg;
         bool live = KW == 1 || v < n_keytiles;
@@ -256,7 +283,7 @@ __global__ __launch_bounds__(NT, TWO ? 4 : 1) void attn_fwd_kernel(FwdArgs a, It
         if (in_prefix) {
           m0 = pk0;
           m1 = walk.k1;
-          causal = 0;
+          causal = own = 0;
           kmax = wave_rows > 0 ? m1 : -1;
         }
         live &= kt + BN > m0;
@@ -267,6 +294,7 @@ __global__ __launch_bounds__(NT, TWO ? 4 : 1) void attn_fwd_kernel(FwdArgs a, It
         m0 = __builtin_amdgcn_readfirstlane(m0);
         m1 = __builtin_amdgcn_readfirstlane(m1);
         causal = __builtin_amdgcn_readfirstlane(causal);
+        own = __builtin_amdgcn_readfirstlane(own);
         kmax = __builtin_amdgcn_readfirstlane(live ? kmax : 0);
         kt = __builtin_amdgcn_readfirstlane(kt);
       }
@@ -316,11 +344,11 @@ __global__ __launch_bounds__(NT, TWO ? 4 : 1) void attn_fwd_kernel(FwdArgs a, It
       if (pf) issue(n + NST - TPB);
 
       // ---- mask (only on edge / diagonal tiles)
-      const bool need_mask = (kt < m0) | (kt + BN > m1) | (causal & (kt + BN - 1 > wr0 + delta));
+      const bool need_mask = (kt < m0) | (kt + BN > m1) | (causal & (kt + BN - 1 > wr0 + delta)) | (FEW && own);
       if (need_mask) {
         // keys [lo, hi) of the lane half's, counted from kt + 8 hh
-        const int lo = m0 - kt - hh * 8;
-        const int hi = (causal ? min(m1, row + delta + 1) : m1) - kt - hh * 8;
+        const int lo = (FEW && own ? own0 : m0) - kt - hh * 8;
+        const int hi = (FEW && own ? own1 : causal ? min(m1, row + delta + 1) : m1) - kt - hh * 8;
 #pragma unroll
         for (int g = 0; g < G; ++g)
 #pragma unroll
@@ -443,10 +471,17 @@ __global__ __launch_bounds__(NT, TWO ? 4 : 1) void attn_fwd_kernel(FwdArgs a, It
   const float inv = has ? 1.f / l_tot : 0.f;
   const float lse_v = has ? (m_run * c2 + __log2f(l_tot)) * kLn2 : neg_inf();
   if (!row_ok) return;
-  const int64_t obase = ((int64_t)row * a.H + head) * D + hh * 4;
+  const int64_t obase = ((int64_t)row * a.H + qhead) * D + hh * 4;
   // element offset of the wavefront's quad i
   auto dim = [&](int i) { return ((kg * NQW + i) >> 2) * 32 + ((kg * NQW + i) & 3) * 8; };
-  if constexpr (!MERGE) {
+  if constexpr (FEW) {
+    const int64_t part = it[1];
+    float* o = a.o_acc + part * a.T_q * a.H * D + obase;
+#pragma unroll
+    for (int i = 0; i < NQW; ++i)
+      *(float4*)(o + dim(i)) = make_float4(acc[i][0] * inv, acc[i][1] * inv, acc[i][2] * inv, acc[i][3] * inv);
+    if (hh == 0 && kg == 0) a.lse_acc[(part * a.H + qhead) * a.T_q + row] = lse_v;
+  } else if constexpr (!MERGE) {
 #pragma unroll
     for (int i = 0; i < NQW; ++i)
       *(u32x2*)(a.o + obase + dim(i)) =
@@ -485,7 +520,77 @@ __global__ __launch_bounds__(NT, TWO ? 4 : 1) void attn_fwd_kernel(FwdArgs a, It
   }
 }
 
+// Merge of the P parts of a call of few rows, one workgroup for each row and head:
+// O = sum_p w_p O_p with w_p = e^(L_p - L), L = log sum_p e^(L_p).  Dummy slots, and
+// rows that no part sees a key of, get O = +0, LSE = -inf.  The parts are read D / 4
+// lanes wide, as many at a time as the threads hold, and summed in a fixed order.
+template <int D>
+__global__ __launch_bounds__(kJoinThreads) void attn_join_kernel(FwdArgs a, int parts, int n_real) {
+  constexpr int L = D / 4, G = kJoinThreads / L;
+  __shared__ float wt[kMaxParts];
+  __shared__ float4 red[G][L];
+  const int row = blockIdx.x, head = blockIdx.y, tid = threadIdx.x, l = tid % L, g = tid / L;
+  const bool real = head < n_real;
+  float m = neg_inf();
+  float mine = neg_inf();
+  if (real && tid < parts) mine = a.lse_acc[((int64_t)tid * a.H + head) * a.T_q + row];
+  __shared__ float wm[kJoinThreads / 64], ws[kJoinThreads / 64];
+  m = mine;
+#pragma unroll
+  for (int off = 32; off >= 1; off >>= 1) m = fmaxf(m, __shfl_xor(m, off));
+  if ((tid & 63) == 0) wm[tid >> 6] = m;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kJoinThreads / 64; ++i) m = fmaxf(m, wm[i]);
+  const float e = mine == neg_inf() ? 0.f : __expf(mine - m);
+  float s = e;
+#pragma unroll
+  for (int off = 32; off >= 1; off >>= 1) s += __shfl_xor(s, off);
+  if ((tid & 63) == 0) ws[tid >> 6] = s;
+  if (tid < kMaxParts) wt[tid] = e;
+  __syncthreads();
+  s = 0.f;
+#pragma unroll
+  for (int i = 0; i < kJoinThreads / 64; ++i) s += ws[i];
+  float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (s > 0.f) {
+    const float* o = a.o_acc + ((int64_t)row * a.H + head) * D + l * 4;
+    const int64_t stride = (int64_t)a.T_q * a.H * D;
+#pragma unroll 8
+    for (int p = g; p < parts; p += G) {
+      const float4 v = *(const float4*)(o + p * stride);
+      const float w = wt[p];
+      x.x += w * v.x; x.y += w * v.y; x.z += w * v.z; x.w += w * v.w;
+    }
+  }
+  red[g][l] = x;
+  __syncthreads();
+  if (g == 0) {
+#pragma unroll
+    for (int i = 1; i < G; ++i) {
+      const float4 v = red[i][l];
+      x.x += v.x; x.y += v.y; x.z += v.z; x.w += v.w;
+    }
+    const float inv = s > 0.f ? 1.f / s : 0.f;
+    *(u32x2*)(a.o + ((int64_t)row * a.H + head) * D + l * 4) = pack_bf16x4(x.x * inv, x.y * inv, x.z * inv, x.w * inv);
+    if (l == 0) a.lse[(int64_t)head * a.T_q + row] = s > 0.f ? m + __logf(s) : neg_inf();
+  }
+}
+
 }  // namespace
+
+hipError_t launch_attn_few(const FwdArgs& a, const ItemList& list, int D, int parts, int n_real, hipStream_t st) {
+  if (a.n_items > 0) {
+    const hipError_t e = D == 128 ? sp_launch(kKFwd, attn_fwd_kernel<128, false, 4, false, true, true>, dim3(a.n_items),
+                                              dim3(NT), st, a, list)
+                                  : sp_launch(kKFwd, attn_fwd_kernel<64, false, 4, false, true, true>, dim3(a.n_items),
+                                              dim3(NT), st, a, list);
+    if (e != hipSuccess) return e;
+  }
+  const dim3 grid(a.T_q, a.H), block(kJoinThreads);
+  return D == 128 ? sp_launch(0, attn_join_kernel<128>, grid, block, st, a, parts, n_real)
+                  : sp_launch(0, attn_join_kernel<64>, grid, block, st, a, parts, n_real);
+}
 
 template <int D, int KW, bool TWO>
 static hipError_t launch_fwd(const FwdArgs& a, const ItemList& list, bool merge, bool prefix, hipStream_t st) {

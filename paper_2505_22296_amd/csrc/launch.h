@@ -139,6 +139,9 @@ struct ReduceArgs {
 //   fwd / dq of a batch with shared prefixes:
 //              {record, 0, 0, 0, 0, head, kv_head, 0}: the record of the item's
 //              first workgroup, in ints from the list's start (layout: RowSlot)
+//   fwd of few rows, shared prefixes:
+//              {record, part, windows, query heads a slot, 0, head, kv_head, 0}: windows,
+//              the place of {own key begin, end} of every row
 //   zero fill of a dummy query slot (fwd / dq): {r_begin, r_end, 0, 0, 0, slot, 0, 2}
 //   zero fill of a KV head no real query head reads (dk/dv):
 //              {k_begin, k_end, 0, 0, 0, 0, kv_head, 3}
@@ -260,6 +263,11 @@ struct LaunchShape {
 // `prefix`: the row items name records (shared prefixes); not with `merge`.
 hipError_t launch_attn_fwd(const FwdArgs& a, const ItemList& list, LaunchShape s, int D, bool merge, bool prefix,
                            hipStream_t st);
+// A shared-prefix forward of few rows: every item one workgroup with a part of the
+// keys, then the merge of the parts (partial results in o_acc, lse_acc: [parts, T_q,
+// H, D], [parts, H, T_q]).
+static constexpr int kMaxParts = 256;
+hipError_t launch_attn_few(const FwdArgs& a, const ItemList& list, int D, int parts, int n_real, hipStream_t st);
 hipError_t launch_attn_dq(const DqArgs& a, const ItemList& list, LaunchShape s, int D, bool prefix, hipStream_t st);
 hipError_t launch_attn_dkdv(const DkdvArgs& a, const ItemList& list, LaunchShape s, int D, hipStream_t st);
 // dQ and dK/dV in one launch; (q.split, k.split) one of (4, 2), (2, 1),

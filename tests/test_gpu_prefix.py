@@ -154,6 +154,34 @@ def test_large_batches_reach_every_launch_shape(sp):
     assert seen["list"] == {True, False}
 
 
+FEW = [  # rows, keys, prefixes, hq, hkv, dummies, D, causal: a long prompt's keys and few rows
+    ([0] + [1] * 16, [20000] + [100 + 7 * i for i in range(16)], [-1] + [0] * 16, 7, 1, 0, 128, True),
+    ([0] + [1] * 16, [20000] + [100 + 7 * i for i in range(16)], [-1] + [0] * 16, 7, 1, 0, 128, False),
+    ([0, 1, 5, 40], [12001, 9, 300, 40], [-1, 0, 0, 0], 4, 2, 0, 64, True),
+    ([0, 1, 1, 0, 1, 1, 2], [9000, 300, 0, 7001, 1, 33, 2], [-1, 0, 0, -1, 3, 3, 3], 3, 3, 1, 64, True),
+    ([0, 1, 3], [16000, 50, 3], [-1, 0, 0], 40, 1, 0, 128, True),   # more query heads than a slot has lanes
+    ([30, 20, 7], [12000, 20, 90], [-1, 0, 0], 28, 4, 0, 128, True),  # the prompt's last rows too
+    ([0] + [1] * 100, [8192] + [1] * 100, [-1] + [0] * 100, 4, 1, 0, 128, True),
+    ([2, 0, 1], [30000, 8000, 1], [-1, -1, 1], 4, 1, 0, 128, True),  # rows without a prefix beside them
+]
+
+
+@pytest.mark.parametrize("nq,nk,pre,hq,hkv,dummies,D,causal", FEW)
+def test_prefix_of_few_rows(sp, nq, nk, pre, hq, hkv, dummies, D, causal):
+    """Keys cut into parts over workgroups, and the parts merged."""
+    d, p = desc(nq, nk, pre, D=D, hq=hq, hkv=hkv, dummies=dummies, causal=causal, pad_q=3 if D == 64 else 0)
+    assert sp.sp_attn_plan(d, sp.SP_OP_FWD)["key_split"] > 1
+    o, lse, *_ = compare(sp, d, p, seed=len(nq))
+    # the same in whole walks (the allocation-free forward never cuts the keys): both
+    # are within P's rounding of each other
+    q, k, v, _ = inputs(d, len(nq))
+    o2, l2 = torch.empty_like(o), torch.empty_like(lse)
+    sp.sp_attn_fwd_static(d, q, k, v, o2, l2)
+    assert (o.float() - o2.float()).abs().max() <= 4 * STEP16 * v.float().abs().max()
+    fin = lse > -math.inf
+    assert torch.equal(fin, l2 > -math.inf) and (lse - l2)[fin].abs().max() <= 1e-4
+
+
 def test_prefix_large_scores(sp):
     """Scores of a few hundred: the running maximum is raised between the prefix's
     keys and the answer's, in either order."""
