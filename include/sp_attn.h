@@ -570,8 +570,8 @@ sp_status sp_policy_loss_bwd(const sp_policy_params* params, const void* logits,
  *
  * q: DEVICE bf16, token t at q + t * q_stride (in elements), its H_q heads of
  * head_dim next to each other; k, v the same with H_kv heads: three tensors, or
- * parts of one projection's output.  Strides are multiples of 8 and hold the
- * heads; every tensor is 16-byte aligned.  positions: DEVICE int32 [T], or NULL:
+ * parts of one projection's output.  Strides are multiples of 8 below 2^26 and hold
+ * the heads; every tensor is 16-byte aligned.  positions: DEVICE int32 [T], or NULL:
  * token t is at position_base + t.  w_q, w_k: DEVICE bf16 [head_dim] or NULL.
  * q_dst: [sp, T, Hq_loc, D]; k_dst, v_dst: [sp, T, Hkv_loc, D] bf16, contiguous,
  * written.  inv_freq and the maps: HOST, read during the call; any finite

@@ -1265,7 +1265,7 @@ sp_status qk_args(const sp_qk_desc* d, spk::QkArgs& a) {
   return SP_OK;
 }
 bool qk_stride_ok(const sp_qk_desc* d, int64_t stride, int H) {
-  return stride % 8 == 0 && stride >= (int64_t)H * d->head_dim && stride < (int64_t(1) << 40);
+  return stride % 8 == 0 && stride >= (int64_t)H * d->head_dim && stride < (int64_t(1) << 26);
 }
 size_t qk_workspace(const spk::QkArgs& a, int D) {
   return align256((size_t)spk::qk_bwd_groups(a, D) * 2 * D * sizeof(float));

@@ -25,8 +25,9 @@
 // depends on the token -- the angles -- is formed once for the whole range, and the
 // next head's loads are in flight while one is worked on.  (Heads on the lanes and
 // one token a wavefront instead: forward of 4096 tokens of 28 / 4 heads to 8 ranks,
-// D = 128, 20.1 us, now 17.9, 5.9 TB/s; backward 32.8 us, now 30.5, of 8191 tokens of
-// 40 / 8 heads from 16 ranks 99, now 72, 5.3 TB/s.)
+// D = 128, 20.1 us, now 17.8, 5.9 TB/s; their backward, with the sum of the weight
+// gradients, 53 us, now 33; of 8191 tokens of 40 / 8 heads from 16 ranks 104 us, now
+// 76, 5.0 TB/s.)
 #include <algorithm>
 #include <type_traits>
 
@@ -55,18 +56,22 @@ SP_DEV void lane_chunks(int l, int rot, int& ca, int& cb) {
   cb = turned ? l + rot / 16 : 2 * l + 1;
 }
 
-// cos and sin (times the scale) of the lane's eight pairs at one position.  The
-// instructions take turns and are off by at most 1.3e-7 (measured over 2^22 values).
+// cos and sin (times the scale) of the lane's eight pairs at one position.  Pairs
+// that are not turned have frequency 0 in the table: cos 1, sin 0, with no branch
+// around a load (the compiler waits for each of eight in turn otherwise: +2 us a
+// kernel).  The instructions take turns and are off by at most 1.3e-7 (measured over
+// 2^22 values).
 template <bool NEIGH, typename A>
 SP_DEV void lane_angles(A a, int l, int64_t pos, float (&cs)[8], float (&sn)[8]) {
+  uint64_t freq[8];
+#pragma unroll
+  for (int k = 0; k < 8; ++k) freq[k] = a->freq[8 * l + k];  // (either pairing)
 #pragma unroll
   for (int k = 0; k < 8; ++k) {
-    const int f = 8 * l + k;  // the pair's frequency (either pairing)
-    const bool turned = f < a->rot / 2;
-    const uint64_t turns = (uint64_t)pos * a->freq[f & 63];
-    const float x = (float)(int32_t)(turns >> 32) * 0x1p-32f;  // in [-1/2, 1/2]
-    cs[k] = turned ? __builtin_amdgcn_cosf(x) * a->rope_scale : 1.f;
-    sn[k] = turned ? __builtin_amdgcn_sinf(x) * a->rope_scale : 0.f;
+    const float x = (float)(int32_t)(((uint64_t)pos * freq[k]) >> 32) * 0x1p-32f;  // in [-1/2, 1/2]
+    const float scale = 8 * l + k < a->rot / 2 ? a->rope_scale : 1.f;
+    cs[k] = __builtin_amdgcn_cosf(x) * scale;
+    sn[k] = __builtin_amdgcn_sinf(x) * scale;
   }
 }
 
@@ -126,6 +131,14 @@ struct QkSpans {
   int q_units, q_span, kv_span;
 };
 
+// Chunk `chunk` of the lane's token in a row of tokens `stride` chunks apart: a
+// uniform base and a 32-bit offset a lane (16 tokens of less than 2^26 elements).
+template <typename P>
+SP_DEV P* lane_chunk(P* base, int tok, int64_t stride, int chunk) {
+  typedef std::conditional_t<std::is_const_v<P>, const char, char> Byte;
+  return (P*)((Byte*)base + ((uint32_t)tok * (uint32_t)stride + (uint32_t)chunk) * 16u);
+}
+
 // Row i of a token's heads: its kind (0 query, 1 key, 2 value), the head, and its
 // entries [s0, s1) in the kind's slot table.
 struct HeadRow {
@@ -137,14 +150,30 @@ SP_DEV HeadRow head_row(A a, int i) {
   const int g = kind == 0 ? i : kind == 1 ? i - a->Hq : i - a->Hq - a->Hkv;
   return HeadRow{kind, g, kind == 0 ? a->q_start[g] : a->kv_start[g], kind == 0 ? a->q_start[g + 1] : a->kv_start[g + 1]};
 }
-// First chunk of token t's row in a [sp, T, H, D] buffer at slot entry e.
+// First chunk of token t0's row in a [sp, T, H, D] buffer at slot entry e, and the
+// chunks from a token to the next.
 template <typename A>
-SP_DEV int64_t slot_chunk(A a, uint32_t e, int kind, int t, int nch) {
+SP_DEV int64_t slot_chunk(A a, uint32_t e, int kind, int t0, int nch) {
   const int H = kind == 0 ? a->Hq_loc : a->Hkv_loc;
-  return (((int64_t)(e >> 10) * a->T + t) * H + (e & 1023)) * nch;
+  return (((int64_t)(e >> 10) * a->T + t0) * H + (e & 1023)) * nch;
+}
+template <typename A>
+SP_DEV int slot_stride(A a, int kind, int nch) {
+  return (kind == 0 ? a->Hq_loc : a->Hkv_loc) * nch;
 }
 template <typename A>
 SP_DEV uint32_t slot_entry(A a, int kind, int s) { return kind == 0 ? a->q_slot[s] : a->kv_slot[s]; }
+
+// Head i's row.
+template <typename A>
+SP_DEV void load_row(A a, int i, int t0, int tok, int ca, int cb, int nch, const u32x4* q, const u32x4* k,
+                     const u32x4* v, u32x4& lo, u32x4& hi) {
+  const HeadRow h = head_row(a, i);
+  const int64_t stride = h.kind == 0 ? a->sq : h.kind == 1 ? a->sk : a->sv;
+  const u32x4* src = (h.kind == 0 ? q : h.kind == 1 ? k : v) + t0 * stride + h.head * nch;
+  lo = *lane_chunk(src, tok, stride, ca);
+  hi = *lane_chunk(src, tok, stride, cb);
+}
 
 // A workgroup's wavefronts take `span` heads each of the tokens of blockIdx.x;
 // behind a token's heads come three rows for the dummy slots of each kind.
@@ -159,30 +188,23 @@ __global__ __launch_bounds__(kQB) void qk_rope_kernel(A args, int span, const u3
   const Arg<A>* a = (const Arg<A>*)__builtin_amdgcn_kernarg_segment_ptr();
   const int lane = threadIdx.x & 63, l = lane % L;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int tt = blockIdx.x * R + lane / L, t = min(tt, a->T - 1);
-  const bool live = tt < a->T;
+  const int t0 = blockIdx.x * R, tok = min(lane / L, a->T - 1 - t0);  // the lane's token is t0 + tok
+  const bool live = lane / L == tok;
   const int heads = a->Hq + 2 * a->Hkv;
   const int r0 = (blockIdx.y * (kQB / 64) + wave) * span, r1 = min(r0 + span, heads + 3);
   if (r0 >= r1) return;
   int ca, cb;
   lane_chunks<NEIGH>(l, a->rot, ca, cb);
   u32x4 lo = {0u, 0u, 0u, 0u}, hi = lo;
-  auto load = [&](int i) {
-    if (i >= min(r1, heads)) return;
-    const HeadRow h = head_row(a, i);
-    const u32x4* src = (h.kind == 0 ? q + t * a->sq : h.kind == 1 ? k + t * a->sk : v + t * a->sv) + h.head * NCH;
-    lo = src[ca];
-    hi = src[cb];
-  };
-  load(r0);
+  if (r0 < heads) load_row(a, r0, t0, tok, ca, cb, NCH, q, k, v, lo, hi);
   float cs[8], sn[8];
-  lane_angles<NEIGH>(a, l, positions ? (int64_t)positions[t] : (int64_t)a->pos_base + t, cs, sn);
+  lane_angles<NEIGH>(a, l, positions ? (int64_t)positions[t0 + tok] : (int64_t)a->pos_base + t0 + tok, cs, sn);
   for (int i = r0; i < r1; ++i) {
     u32x4 out_lo = lo, out_hi = hi;
     HeadRow h;
     if (i < heads) {
       h = head_row(a, i);
-      load(i + 1);
+      if (i + 1 < min(r1, heads)) load_row(a, i + 1, t0, tok, ca, cb, NCH, q, k, v, lo, hi);
       if (h.kind < 2) {
         float x[16];
         unpack16(out_lo, out_hi, x);
@@ -207,10 +229,10 @@ __global__ __launch_bounds__(kQB) void qk_rope_kernel(A args, int span, const u3
     }
     u32x4* dst = h.kind == 0 ? q_dst : h.kind == 1 ? k_dst : v_dst;
     for (int s = h.s0; s < h.s1; ++s) {
-      u32x4* p = dst + slot_chunk(a, slot_entry(a, h.kind, s), h.kind, t, NCH);
+      u32x4* p = dst + slot_chunk(a, slot_entry(a, h.kind, s), h.kind, t0, NCH);
       if (live) {
-        st_stream(out_lo, &p[ca]);
-        st_stream(out_hi, &p[cb]);
+        st_stream(out_lo, lane_chunk(p, tok, slot_stride(a, h.kind, NCH), ca));
+        st_stream(out_hi, lane_chunk(p, tok, slot_stride(a, h.kind, NCH), cb));
       }
     }
   }
@@ -218,21 +240,22 @@ __global__ __launch_bounds__(kQB) void qk_rope_kernel(A args, int span, const u3
 
 // Head i's gradient at its first slot, and its row where there is a norm.
 template <typename A>
-SP_DEV void load_grad(A a, int i, int t, int ca, int cb, int nch, const u32x4* q, const u32x4* k,
+SP_DEV void load_grad(A a, int i, int t0, int tok, int ca, int cb, int nch, const u32x4* q, const u32x4* k,
                       const u32x4* dq_src, const u32x4* dk_src, const u32x4* dv_src, const u32x4* w_q,
                       const u32x4* w_k, u32x4& glo, u32x4& ghi, u32x4& xlo, u32x4& xhi) {
   const HeadRow h = head_row(a, i);
   glo = ghi = u32x4{0u, 0u, 0u, 0u};
   if (h.s0 < h.s1) {
     const u32x4* p = (h.kind == 0 ? dq_src : h.kind == 1 ? dk_src : dv_src) +
-                     slot_chunk(a, slot_entry(a, h.kind, h.s0), h.kind, t, nch);
-    glo = ld_stream(&p[ca]);
-    ghi = ld_stream(&p[cb]);
+                     slot_chunk(a, slot_entry(a, h.kind, h.s0), h.kind, t0, nch);
+    glo = ld_stream(lane_chunk(p, tok, slot_stride(a, h.kind, nch), ca));
+    ghi = ld_stream(lane_chunk(p, tok, slot_stride(a, h.kind, nch), cb));
   }
   if (h.kind == 0 ? w_q != nullptr : h.kind == 1 && w_k != nullptr) {
-    const u32x4* xs = (h.kind == 0 ? q + t * a->sq : k + t * a->sk) + h.head * nch;
-    xlo = xs[ca];
-    xhi = xs[cb];
+    const int64_t stride = h.kind == 0 ? a->sq : a->sk;
+    const u32x4* xs = (h.kind == 0 ? q : k) + t0 * stride + h.head * nch;
+    xlo = *lane_chunk(xs, tok, stride, ca);
+    xhi = *lane_chunk(xs, tok, stride, cb);
   }
 }
 
@@ -268,56 +291,57 @@ __global__ __launch_bounds__(kQB, 4) void qk_rope_bwd_kernel(A args, QkStrides o
     whi = w[cb];
   }
   for (int t0 = blockIdx.x * R; t0 < a->T && r0 < r1; t0 += gridDim.x * R) {
-    const int tt = t0 + lane / L, t = min(tt, a->T - 1);
-    const bool live = tt < a->T;
+    const int tok = min(lane / L, a->T - 1 - t0);  // the lane's token is t0 + tok
+    const bool live = lane / L == tok;
     u32x4 glo, ghi, xlo, xhi;  // head i's gradient at its first slot, and its row
-    load_grad(a, r0, t, ca, cb, NCH, q, k, dq_src, dk_src, dv_src, w_q, w_k, glo, ghi, xlo, xhi);
+    load_grad(a, r0, t0, tok, ca, cb, NCH, q, k, dq_src, dk_src, dv_src, w_q, w_k, glo, ghi, xlo, xhi);
     float cs[8], sn[8];
-    lane_angles<NEIGH>(a, l, positions ? (int64_t)positions[t] : (int64_t)a->pos_base + t, cs, sn);
+    lane_angles<NEIGH>(a, l, positions ? (int64_t)positions[t0 + tok] : (int64_t)a->pos_base + t0 + tok, cs, sn);
     for (int i = r0; i < r1; ++i) {
       const HeadRow h = head_row(a, i);
       const u32x4 x0 = xlo, x1 = xhi;
       float c[16];
       unpack16(glo, ghi, c);
-      if (i + 1 < r1) load_grad(a, i + 1, t, ca, cb, NCH, q, k, dq_src, dk_src, dv_src, w_q, w_k, glo, ghi, xlo, xhi);
+      if (i + 1 < r1) load_grad(a, i + 1, t0, tok, ca, cb, NCH, q, k, dq_src, dk_src, dv_src, w_q, w_k, glo, ghi, xlo, xhi);
       for (int s = h.s0 + 1; s < h.s1; ++s) {
         const u32x4* p = (h.kind == 0 ? dq_src : h.kind == 1 ? dk_src : dv_src) +
-                         slot_chunk(a, slot_entry(a, h.kind, s), h.kind, t, NCH);
+                         slot_chunk(a, slot_entry(a, h.kind, s), h.kind, t0, NCH);
+        const int stride = slot_stride(a, h.kind, NCH);
         float y[16];
-        unpack16(ld_stream(&p[ca]), ld_stream(&p[cb]), y);
+        unpack16(ld_stream(lane_chunk(p, tok, stride, ca)), ld_stream(lane_chunk(p, tok, stride, cb)), y);
 #pragma unroll
         for (int d = 0; d < 16; ++d) c[d] += y[d];
       }
-      u32x4* out = (h.kind == 0 ? dq + t * o.q : h.kind == 1 ? dk + t * o.k : dv + t * o.v) + h.head * NCH;
+      const int64_t ostride = h.kind == 0 ? o.q : h.kind == 1 ? o.k : o.v;
+      u32x4* out = (h.kind == 0 ? dq : h.kind == 1 ? dk : dv) + t0 * ostride + h.head * NCH;
       if (h.kind < 2) {
         turn<NEIGH>(c, cs, sn, -1.f);
         if (w) {
-          float x[16], wt[16];
+          float x[16];
           unpack16(x0, x1, x);
+          float ss = 0.f, cx = 0.f;
+#pragma unroll
+          for (int d = 0; d < 16; ++d) ss = __builtin_fmaf(x[d], x[d], ss);
+          const float r = rsqrtf(row_sum<L>(ss) * (1.f / D) + a->eps), rl = live ? r : 0.f;
           // the weights stay packed (8 registers less; four wavefronts a SIMD)
           u32x4 w0 = wlo, w1 = whi;
           asm volatile("" : "+v"(w0), "+v"(w1));
+          float wt[16];
           unpack16(w0, w1, wt);
-          float ss = 0.f, cx = 0.f;
-#pragma unroll
-          for (int d = 0; d < 16; ++d) wt[d] = c[d] * (wt[d] + a->w_off);  // gradient of the normed row
-#pragma unroll
-          for (int d = 0; d < 16; ++d) {
-            ss = __builtin_fmaf(x[d], x[d], ss);
-            cx = __builtin_fmaf(wt[d], x[d], cx);
-          }
-          const float r = rsqrtf(row_sum<L>(ss) * (1.f / D) + a->eps);
-          const float m = row_sum<L>(cx) * r * r * (1.f / D), rl = live ? r : 0.f;
 #pragma unroll
           for (int d = 0; d < 16; ++d) {
             acc[d] = __builtin_fmaf(c[d], x[d] * rl, acc[d]);
-            c[d] = r * (wt[d] - x[d] * m);
+            c[d] *= wt[d] + a->w_off;  // the gradient of the normed row
+            cx = __builtin_fmaf(c[d], x[d], cx);
           }
+          const float m = row_sum<L>(cx) * r * r * (1.f / D);
+#pragma unroll
+          for (int d = 0; d < 16; ++d) c[d] = r * (c[d] - x[d] * m);
         }
       }
       if (live) {
-        st_stream(pack_lo(c), &out[ca]);
-        st_stream(pack_hi(c), &out[cb]);
+        st_stream(pack_lo(c), lane_chunk(out, tok, ostride, ca));
+        st_stream(pack_hi(c), lane_chunk(out, tok, ostride, cb));
       }
     }
   }
@@ -381,7 +405,7 @@ QkGrid qk_grid(int T, int D, int rows, int waves) {
   const int R = 64 / (D / 16), groups = std::max(1, (T + R - 1) / R);
   return QkGrid{groups, std::max(1, std::min((rows + 3) / 4, waves / 4 / groups))};
 }
-constexpr int kQkFwdWaves = 8192, kQkBwdWaves = 4096;
+constexpr int kQkFwdWaves = 4096, kQkBwdWaves = 4096;
 // Workgroups of the backward, which keep a partial weight gradient each.
 QkGrid qk_bwd_grid(const QkArgs& a, int D) {
   QkGrid g = qk_grid(a.T, D, a.Hq + 2 * a.Hkv, kQkBwdWaves);

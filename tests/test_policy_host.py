@@ -153,6 +153,7 @@ def test_qk_calls_refuse_before_launch():
     for i in (1, 3, 5):
         assert fwd(**{f"_{i}": 184}) == sp.SP_ERR_INVALID_ARG       # the heads do not fit
         assert fwd(**{f"_{i}": 196}) == sp.SP_ERR_INVALID_ARG       # not a multiple of 8
+        assert fwd(**{f"_{i}": 1 << 26}) == sp.SP_ERR_INVALID_ARG   # past 32-bit offsets
     for i in (7, 8):
         assert fwd(**{f"_{i}": FAKE + 2}) == sp.SP_ERR_INVALID_ARG
     bwd_ok = [FAKE, 192, FAKE, 192, FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, 192, FAKE, 192, FAKE, 192, FAKE, FAKE,
