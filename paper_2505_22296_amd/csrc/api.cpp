@@ -702,35 +702,24 @@ std::vector<int32_t> merged_items(const std::vector<Item>& rows, const std::vect
 }
 
 // A shared-prefix forward of few rows: tiles of two slots, whose keys are cut into
-// `parts`.  Taken where the model sees a fifth less time in it than in whole walks: a
-// workgroup of a part takes kStartUs and its stages of four key tiles, kFewStageUs
-// each, and the merge kFewJoinUs.  (16 answers of one row to 32768 keys, 7 heads:
-// 313 -> 36 us; one answer, 4 heads, 331 -> 30.)
-constexpr double kFewStageUs = 1.6, kFewJoinUs = 8;
+// `parts`.  Taken where the model sees a fifth less time in it than in whole walks -- a
+// workgroup takes kStartUs and its stages of four key tiles, kFewStageUs each, and the
+// merge kFewJoinUs and the partial results' way out and back -- and where tiles and
+// windows fit the launch's own list: a copy of them would take longer than it gains
+// (a prompt of 1689 rows and 13 answers of 39, copied, 37 us, in whole walks 23).  16
+// answers of one row to 32768 keys, 7 heads: 313 -> 21 us; 64 answers to 8192 keys, 4 heads, 84 -> 19.
+constexpr double kFewStageUs = 1.6, kFewJoinUs = 8, kFewBytesUs = 2e6;
 constexpr int kFewSlots = 2, kFewSplit = kSlots / kFewSlots;
-constexpr int64_t kFewBytes = int64_t(64) << 20;  // of partial results, at most
-struct FewTile {
-  int row0, row1, heads;  // rows of both slots, query heads a slot
-  int prefix, own0, own1;  // and the keys that some row sees
-  int head, kv;
-};
 struct FewPlan {
   int parts = 0;  // 0: not taken
-  std::vector<FewTile> tiles;
+  std::vector<spk::FewTile> tiles;
   std::vector<int32_t> windows;  // own keys [begin, end) of every row
 };
-int few_tile_steps(const Problem& p, const FewTile& t, int BN) {
-  auto steps = [&](int a, int b) { return b > a ? (b - (a & ~7) + BN - 1) / BN : 0; };
-  return (t.prefix >= 0 ? steps(p.segs[t.prefix].ka, p.segs[t.prefix].kb) : 0) + steps(t.own0, t.own1);
-}
 // `whole_us`: the model's time of the launch without parts.
 FewPlan few_plan(const sp_attn_desc* d, const Problem& p, double whole_us) {
+  constexpr size_t kInts = std::size(decltype(spk::ItemList::v){});
   FewPlan f;
-  // (a tile holds 64 rows of a head, or fewer: more rows leave no CUs for parts)
-  if (p.prefix.empty() || p.n_real == 0 || whole_us < 2 * (kStartUs + kFewJoinUs) ||
-      (int64_t)d->T_q * p.n_real > (int64_t)kCus / 2 * kFewSlots * kSlotRows ||
-      (int64_t)2 * d->T_q * d->H_loc * (p.D + 1) * 4 > kFewBytes)
-    return f;
+  if (p.prefix.empty() || p.n_real == 0 || d->T_q == 0 || (size_t)2 * d->T_q > kInts) return f;
   std::vector<int> prefix(d->T_q, -1);
   f.windows.assign((size_t)2 * d->T_q, 0);
   for (size_t s = 0; s < p.segs.size(); ++s) {
@@ -752,73 +741,31 @@ FewPlan few_plan(const sp_attn_desc* d, const Problem& p, double whole_us) {
       for (int i = 0; i < d->T_q;) {
         int e = i + 1;
         while (e < d->T_q && e < i + rows && prefix[e] == prefix[i]) ++e;
-        FewTile t{i, e, heads, prefix[i], 0, 0, h0, kv};
+        spk::FewTile t{i, e, 0, 0, 0, 0, h0 | heads << 16, kv};
+        if (prefix[i] >= 0) {
+          t.p0 = p.segs[prefix[i]].ka;
+          t.p1 = p.segs[prefix[i]].kb;
+        }
         for (int r = i; r < e; ++r) {
           const int a = f.windows[2 * r], z = f.windows[2 * r + 1];
           if (z <= a) continue;
-          t.own0 = t.own1 > t.own0 ? std::min(t.own0, a) : a;
-          t.own1 = std::max(t.own1, z);
+          t.k0 = t.k1 > t.k0 ? std::min(t.k0, a) : a;
+          t.k1 = std::max(t.k1, z);
         }
-        longest = std::max(longest, few_tile_steps(p, t, BN));
+        longest = std::max(longest, spk::few_steps(t.p0, t.p1, BN) + spk::few_steps(t.k0, t.k1, BN));
         f.tiles.push_back(t);
         i = e;
       }
     }
   }
+  if (f.tiles.size() * kItemInts + f.windows.size() > kInts) return f;
   const int stages = (longest + kFewSplit - 1) / kFewSplit;  // of four tiles
-  const int64_t n = (int64_t)f.tiles.size(), room = kFewBytes / ((int64_t)d->T_q * d->H_loc * (p.D + 1) * 4);
-  const int parts = (int)std::min<int64_t>({(int64_t)kCus / std::max<int64_t>(n, 1), stages / 2, room, spk::kMaxParts});
+  const int parts = (int)std::min<size_t>({kCus / f.tiles.size(), (size_t)stages / 2, (size_t)spk::kMaxParts});
   if (parts < 2) return f;
-  const double us = kStartUs + (double)((stages + parts - 1) / parts) * kFewStageUs + kFewJoinUs;
+  const double us = kStartUs + (double)((stages + parts - 1) / parts) * kFewStageUs + kFewJoinUs +
+                    2.0 * parts * d->T_q * d->H_loc * p.D * 4 / kFewBytesUs;
   if (us < 0.8 * whole_us) f.parts = parts;
   return f;
-}
-// The items, their records and the rows' windows as one list.
-std::vector<int32_t> few_list(const sp_attn_desc* d, const Problem& p, const FewPlan& f) {
-  const int BN = spk::fwd_tile_keys(p.D, kFewSplit), ints = spk::record_ints(kFewSlots);
-  const size_t n = f.tiles.size() * f.parts, windows = n * (kItemInts + ints);
-  std::vector<int32_t> out(windows, 0);
-  for (size_t i = 0; i < n; ++i) {
-    // eight parts at a time, the tiles of each on one XCD (i % 8): they share keys
-    const size_t block = i / (kXcds * f.tiles.size()) * kXcds, width = std::min<size_t>(kXcds, f.parts - block);
-    const size_t in = i - block * f.tiles.size();
-    const FewTile& t = f.tiles[in / width];
-    const int part = (int)(block + in % width);
-    const int32_t item[kItemInts] = {(int32_t)(n * kItemInts + i * ints), part, (int32_t)windows, t.heads, 0, t.head, t.kv, 0};
-    std::copy(item, item + kItemInts, &out[i * kItemInts]);
-    int32_t* r = &out[n * kItemInts + i * ints];
-    const int all = few_tile_steps(p, t, BN);
-    const int v0 = (int)((int64_t)all * part / f.parts), v1 = (int)((int64_t)all * (part + 1) / f.parts);
-    int at = 0, n_ranges = 0, tiles = 0;
-    auto range = [&](int k0, int k1, bool prefix) {
-      if (k1 <= k0) return;
-      const int first = k0 & ~7, steps = (k1 - first + BN - 1) / BN;
-      const int a = std::max(v0, at), b = std::min(v1, at + steps);
-      if (b > a) {
-        tiles += b - a;
-        int32_t* o = r + spk::kRecordRanges + 3 * n_ranges++;
-        o[0] = tiles;
-        o[1] = first + (a - at) * BN;
-        o[2] = std::min(k1, first + (b - at) * BN);
-        if (prefix) r[1] = k0, r[2] = 1;
-      }
-      at += steps;
-    };
-    if (t.prefix >= 0) range(p.segs[t.prefix].ka, p.segs[t.prefix].kb, true);
-    range(t.own0, t.own1, false);
-    r[0] = tiles;
-    const int rows = kSlotRows / t.heads;
-    for (int s = 0; s < kFewSlots; ++s) {
-      int32_t* o = r + spk::kRecordRanges + 3 * (1 + kFewSlots) + 5 * s;
-      o[0] = std::min(t.row1, t.row0 + s * rows);
-      o[1] = std::min(t.row1, t.row0 + (s + 1) * rows);
-      o[2] = t.own0;
-      o[3] = t.own1;
-      if (o[1] <= o[0]) o[0] = o[1] = t.row0;  // (a row that exists, for addresses)
-    }
-  }
-  out.insert(out.end(), f.windows.begin(), f.windows.end());
-  return out;
 }
 
 // Zero fills as work items of the same launch (no extra kernels): dummy
@@ -864,7 +811,7 @@ int n_unread_kv(const sp_attn_desc* d, const Problem& p) {
 // Workspace layout.
 struct Layout {
   size_t items_dq = 0, items_kv = 0, neg_d = 0, lse2 = 0, part_k = 0, part_v = 0, total = 0;
-  size_t few_items = 0, few_o = 0, few_lse = 0;  // a forward of few rows
+  size_t few_o = 0, few_lse = 0;  // a forward of few rows
 };
 
 size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
@@ -898,12 +845,11 @@ Layout layout_for(const sp_attn_desc* d, const Problem& p, int op, size_t n_item
   return L;
 }
 
-// Workspace of a shared-prefix forward of few rows.
+// Workspace of a shared-prefix forward of few rows: the partial results.
 Layout layout_few(const sp_attn_desc* d, const Problem& p, const FewPlan& f) {
   Layout L;
   const size_t rows = (size_t)f.parts * d->T_q * d->H_loc;
-  L.few_o = align256(f.tiles.size() * f.parts * (kItemInts + spk::record_ints(kFewSlots)) * 4 + f.windows.size() * 4);
-  L.few_lse = L.few_o + align256(rows * p.D * 4);
+  L.few_lse = align256(rows * p.D * 4);
   L.total = L.few_lse + align256(rows * 4);
   return L;
 }
@@ -1460,22 +1406,18 @@ static sp_status fwd_few(const sp_attn_desc* d, const Problem& p, const FewPlan&
   sp_status s = check_ws(L, ws, ws_bytes);
   if (s != SP_OK) return s;
   if ((s = refuse_capture(st)) != SP_OK) return s;
-  const std::vector<int32_t> items = few_list(d, p, few);
   spk::FwdArgs a{};
   spk::ItemList list{};
-  if (items.size() <= std::size(list.v)) {
-    std::copy(items.begin(), items.end(), list.v);
-  } else {
-    if ((s = upload(at(ws, L.few_items), items, st)) != SP_OK) return s;
-    a.items = (const int32_t*)at(ws, L.few_items);
-  }
+  std::memcpy(list.v, few.tiles.data(), few.tiles.size() * sizeof(spk::FewTile));
+  std::copy(few.windows.begin(), few.windows.end(), list.v + few.tiles.size() * kItemInts);
   a.q = (const uint16_t*)q; a.k = (const uint16_t*)k; a.v = (const uint16_t*)v;
   a.o = (uint16_t*)o; a.lse = lse;
   a.o_acc = (float*)at(ws, L.few_o); a.lse_acc = (float*)at(ws, L.few_lse);
   a.T_q = d->T_q; a.T_k = d->T_k; a.H = d->H_loc; a.Hkv = d->Hkv_loc;
   a.scale_log2 = d->softmax_scale * 1.4426950408889634f;
-  a.n_items = (int)(few.tiles.size() * few.parts);
-  SP_HIP(spk::launch_attn_few(a, list, p.D, few.parts, p.n_real, st));
+  a.n_items = (int)few.tiles.size();
+  a.parts = few.parts;
+  SP_HIP(spk::launch_attn_few(a, list, p.D, p.n_real, st));
   return SP_OK;
 }
 

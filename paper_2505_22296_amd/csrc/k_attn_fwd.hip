@@ -80,18 +80,14 @@ struct FwdStage {
 // PFX: segments share prefixes; the items name records of slots and key ranges
 // (dev_common.h), the workgroup's rows come from several segments.
 // FEW (with PFX, KW = 4): a call of few rows, whose items would leave most CUs idle
-// behind long walks.  An item is one workgroup with two slots and a part of their
-// keys; a slot holds 32 / g rows for each of the g query heads that share a KV head
-// (lane i: row i / g, head i % g; a token an answer then still fills a slot), of any
-// segments of one prefix, so that the own keys are a window per lane; the part's
-// normalised result goes to float32 buffers that attn_join_kernel merges.
-// (the list where it lies in the kernel arguments, for lanes' own indexes; the
-// second argument of the kernel, behind the first without a gap)
-static_assert(sizeof(FwdArgs) % alignof(ItemList) == 0, "the list follows the arguments");
+// behind long walks.  The list holds tiles of two slots (FewTile) and the rows'
+// windows; workgroup b takes one part of one tile's key tiles, eight parts at a time
+// so that a part's tiles, which share keys, are on one XCD (b % 8).  A slot holds 32 /
+// g rows for each of the g query heads that share a KV head (lane i: row i / g, head
+// i % g; a token an answer then still fills a slot), of any segments of one prefix, so
+// that the own keys are a window per lane; the part's normalised result goes to
+// float32 buffers that attn_join_kernel merges.
 typedef const __attribute__((address_space(4))) int32_t* TablePtr;
-SP_DEV TablePtr few_rows_table(const FwdArgs& a, TablePtr list) {
-  return a.items ? (TablePtr)a.items : list;
-}
 template <int D, bool MERGE, int KW, bool TWO, bool PFX, bool FEW = false>
 __global__ __launch_bounds__(NT, TWO ? 4 : 1) void attn_fwd_kernel(FwdArgs a, ItemList list) {
   using S = FwdStage<D, KW>;
@@ -103,23 +99,37 @@ __global__ __launch_bounds__(NT, TWO ? 4 : 1) void attn_fwd_kernel(FwdArgs a, It
 
   __shared__ u32x4 smem[S::SMEM];
 
-  int pos = blockIdx.x, sub = 0;
-  if constexpr (!FEW)
+  static_assert(sizeof(FwdArgs) % alignof(ItemList) == 0, "the list follows the arguments");
+  const TablePtr table = (TablePtr)__builtin_amdgcn_kernarg_segment_ptr() + sizeof(FwdArgs) / 4;  // FEW
+  int pos, sub = 0, part = 0;
+  if constexpr (FEW) {
+    // (divisions happen in vector registers: back to scalar ones)
+    const int first = __builtin_amdgcn_readfirstlane(blockIdx.x / (8 * a.n_items) * 8);
+    const int width = min(8, a.parts - first), in = blockIdx.x - first * a.n_items;
+    pos = __builtin_amdgcn_readfirstlane(in / width);
+    part = first + in - pos * width;
+  } else {
     if (!split_pos<KW>(blockIdx.x, a.n_items, pos, sub)) return;
+  }
   int32_t it[kItemInts];
-  load_item(a.items, list, 0, pos, it);
+  if constexpr (FEW) {
+#pragma unroll
+    for (int j = 0; j < kItemInts; ++j) it[j] = __builtin_amdgcn_readfirstlane(table[pos * kItemInts + j]);
+  } else {
+    load_item(a.items, list, 0, pos, it);
+  }
   static_assert(!PFX || !MERGE, "a ring step has no shared prefixes");
   static_assert(!FEW || (PFX && KW == 4), "few rows");
   int q0 = it[0], q1 = it[1], k1 = it[3];
   int k0 = it[2], delta = it[4];
-  const int head = it[5], kvh = it[6];
+  const int head = FEW ? it[6] & 0xffff : it[5], kvh = FEW ? it[7] : it[6];
   const int tid = threadIdx.x;
-  if constexpr (KW > 1) {
+  if constexpr (KW > 1 && !FEW) {
     if (!PFX || it[7] == kItemFillQ)
       if (!split_rows<KW>(it[7] == kItemFillQ, 32 * RW, sub, q0, q1)) return;
     if (!PFX && a.causal) k1 = max(k0, min(k1, q1 + delta));
   }
-  if (it[7] == kItemFillQ) {
+  if (!FEW && it[7] == kItemFillQ) {
     // dummy slot: O = +0, LSE = -inf (ring: the accumulators' identity on the
     // first chunk, and +0 in the bf16 copy)
     if constexpr (!MERGE) {
@@ -137,10 +147,27 @@ __global__ __launch_bounds__(NT, TWO ? 4 : 1) void attn_fwd_kernel(FwdArgs a, It
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lane = tid & 63, hh = lane >> 5, l32 = lane & 31;
   const int rg = KW > 1 ? w % RW : w, kg = KW > 1 ? w / RW : 0;
-  const int record = it[0] + sub * record_ints(RW);  // PFX
+  const int record = it[0] + sub * record_ints(RW);  // PFX, not FEW
   int pk0 = 0;
   bool has_prefix = false;
-  if constexpr (PFX) {
+  const int g = FEW ? it[6] >> 16 : 1;  // query heads in a slot
+  // FEW: key tiles of the prefix and of all, the first of the part
+  int pk1 = 0, n_pre = 0, v0 = 0, n_keytiles = 0;
+  if constexpr (FEW) {
+    pk0 = it[2];
+    pk1 = it[3];
+    k0 = it[4];
+    k1 = it[5];
+    n_pre = few_steps(pk0, pk1, BN);
+    const int all = n_pre + few_steps(k0, k1, BN);
+    const int each = __builtin_amdgcn_readfirstlane(all / a.parts), more = all - each * a.parts;
+    v0 = part * each + min(part, more);
+    n_keytiles = each + (part < more);
+    const int rows = __builtin_amdgcn_readfirstlane(32 / g);
+    q0 = it[0] + rg * rows;
+    q1 = min(it[1], q0 + rows);
+    if (q0 >= q1) q0 = q1 = it[0];  // (a row that exists, for addresses)
+  } else if constexpr (PFX) {
     const RowSlot slot = load_slot(a.items, list, record, RW, rg);
     q0 = slot.row0;
     q1 = slot.row1;
@@ -151,14 +178,12 @@ __global__ __launch_bounds__(NT, TWO ? 4 : 1) void attn_fwd_kernel(FwdArgs a, It
     has_prefix = table_at(a.items, list, record + 2) != 0;
   }
   const int wr0 = PFX ? q0 : q0 + rg * 32;  // the wavefront's first row
-  const int g = FEW ? it[3] : 1;            // query heads in a slot
   const int row = wr0 + (FEW ? l32 / g : l32);
-  const bool row_ok = FEW ? row < q1 && l32 < 32 / g * g : row < q1;
+  const bool row_ok = row < q1;
   const int qhead = FEW ? head + l32 % g : head;
   int own0 = 0, own1 = 0;  // FEW: the row's window of its own segment's keys
   if constexpr (FEW) {
-    const TablePtr args = (TablePtr)__builtin_amdgcn_kernarg_segment_ptr();
-    const TablePtr win = few_rows_table(a, args + sizeof(FwdArgs) / 4) + it[2] + 2 * (row_ok ? row : q0);
+    const TablePtr win = table + a.n_items * kItemInts + 2 * (row_ok ? row : q0);
     own0 = win[0];
     own1 = win[1];
   }
@@ -193,8 +218,7 @@ __global__ __launch_bounds__(NT, TWO ? 4 : 1) void attn_fwd_kernel(FwdArgs a, It
 
   const int kt_first = k0 & ~7;
   // stages of KW tiles (PFX: of the record's key tiles)
-  int n_keytiles = 0;
-  if constexpr (PFX) n_keytiles = table_at(a.items, list, record);
+  if constexpr (PFX && !FEW) n_keytiles = table_at(a.items, list, record);
   const int n_tiles = PFX ? (n_keytiles + KW - 1) / KW : (k1 > k0) ? (k1 - kt_first + BN * KW - 1) / (BN * KW) : 0;
   KeyWalk walk_in, walk;  // of the copies and of the tiles in use
 
@@ -213,14 +237,24 @@ __global__ __launch_bounds__(NT, TWO ? 4 : 1) void attn_fwd_kernel(FwdArgs a, It
   const uint16_t* kbase = a.k + (int64_t)kvh * D;
   const uint16_t* vbase = a.v + (int64_t)kvh * D;
   const int kend = k1;
+  // FEW: the part's first key tile, and what changes behind the prefix
+  const int few_kt = (pk0 & ~7) + v0 * BN, few_skip = (k0 & ~7) - (pk0 & ~7) - n_pre * BN, few_end = kend - pk1;
   auto issue = [&](int n) {
     int kt = kt_first + (n * KW + kg) * BN, k1 = kend;
     if constexpr (PFX) {
       const int v = n * KW + kg;
       if (KW > 1 && v >= n_keytiles) return;
-      walk_in.seek(a.items, list, record, v);
-      kt = walk_in.kt0 + (v - walk_in.v0) * BN;
-      k1 = walk_in.k1;
+      if constexpr (FEW) {
+        // (selected by arithmetic: as ?: the compiler selects between captured
+        // addresses and keeps the values in scratch memory)
+        const int behind = v0 + v < n_pre ? 0 : -1;
+        kt = few_kt + v * BN + (behind & few_skip);
+        k1 = pk1 + (behind & few_end);
+      } else {
+        walk_in.seek(a.items, list, record, v);
+        kt = walk_in.kt0 + (v - walk_in.v0) * BN;
+        k1 = walk_in.k1;
+      }
     }
     if (KW > 1 && kt >= k1) return;  // the key group has no tile in the last stage
     u32x4* stg = smem + (n % NST) * STAGE + kg * S::TILE + rg * 64;
@@ -277,12 +311,18 @@ __global__ __launch_bounds__(NT, TWO ? 4 : 1) void attn_fwd_kernel(FwdArgs a, It
       if constexpr (PFX) {
         const int v = n * KW + kg;
         bool live = KW == 1 || v < n_keytiles;
-        if (live) walk.seek(a.items, list, record, v);
-        kt = walk.kt0 + (v - walk.v0) * BN;
-        const bool in_prefix = has_prefix & (walk.range == 0);  // visible to every row
+        bool in_prefix;  // visible to every row
+        if constexpr (FEW) {
+          in_prefix = v0 + v < n_pre;
+          kt = few_kt + v * BN + (in_prefix ? 0 : few_skip);
+        } else {
+          if (live) walk.seek(a.items, list, record, v);
+          kt = walk.kt0 + (v - walk.v0) * BN;
+          in_prefix = has_prefix & (walk.range == 0);
+        }
         if (in_prefix) {
           m0 = pk0;
-          m1 = walk.k1;
+          m1 = FEW ? pk1 : walk.k1;
           causal = own = 0;
           kmax = wave_rows > 0 ? m1 : -1;
         }
@@ -475,12 +515,11 @@ __global__ __launch_bounds__(NT, TWO ? 4 : 1) void attn_fwd_kernel(FwdArgs a, It
   // element offset of the wavefront's quad i
   auto dim = [&](int i) { return ((kg * NQW + i) >> 2) * 32 + ((kg * NQW + i) & 3) * 8; };
   if constexpr (FEW) {
-    const int64_t part = it[1];
-    float* o = a.o_acc + part * a.T_q * a.H * D + obase;
+    float* o = a.o_acc + (int64_t)part * a.T_q * a.H * D + obase;
 #pragma unroll
     for (int i = 0; i < NQW; ++i)
       *(float4*)(o + dim(i)) = make_float4(acc[i][0] * inv, acc[i][1] * inv, acc[i][2] * inv, acc[i][3] * inv);
-    if (hh == 0 && kg == 0) a.lse_acc[(part * a.H + qhead) * a.T_q + row] = lse_v;
+    if (hh == 0 && kg == 0) a.lse_acc[((int64_t)part * a.H + qhead) * a.T_q + row] = lse_v;
   } else if constexpr (!MERGE) {
 #pragma unroll
     for (int i = 0; i < NQW; ++i)
@@ -520,12 +559,13 @@ __global__ __launch_bounds__(NT, TWO ? 4 : 1) void attn_fwd_kernel(FwdArgs a, It
   }
 }
 
-// Merge of the P parts of a call of few rows, one workgroup for each row and head:
+// Merge of the parts of a call of few rows, one workgroup for each row and head:
 // O = sum_p w_p O_p with w_p = e^(L_p - L), L = log sum_p e^(L_p).  Dummy slots, and
 // rows that no part sees a key of, get O = +0, LSE = -inf.  The parts are read D / 4
 // lanes wide, as many at a time as the threads hold, and summed in a fixed order.
 template <int D>
-__global__ __launch_bounds__(kJoinThreads) void attn_join_kernel(FwdArgs a, int parts, int n_real) {
+__global__ __launch_bounds__(kJoinThreads) void attn_join_kernel(FwdArgs a, int n_real) {
+  const int parts = a.parts;
   constexpr int L = D / 4, G = kJoinThreads / L;
   __shared__ float wt[kMaxParts];
   __shared__ float4 red[G][L];
@@ -579,17 +619,14 @@ __global__ __launch_bounds__(kJoinThreads) void attn_join_kernel(FwdArgs a, int 
 
 }  // namespace
 
-hipError_t launch_attn_few(const FwdArgs& a, const ItemList& list, int D, int parts, int n_real, hipStream_t st) {
-  if (a.n_items > 0) {
-    const hipError_t e = D == 128 ? sp_launch(kKFwd, attn_fwd_kernel<128, false, 4, false, true, true>, dim3(a.n_items),
-                                              dim3(NT), st, a, list)
-                                  : sp_launch(kKFwd, attn_fwd_kernel<64, false, 4, false, true, true>, dim3(a.n_items),
-                                              dim3(NT), st, a, list);
-    if (e != hipSuccess) return e;
-  }
-  const dim3 grid(a.T_q, a.H), block(kJoinThreads);
-  return D == 128 ? sp_launch(0, attn_join_kernel<128>, grid, block, st, a, parts, n_real)
-                  : sp_launch(0, attn_join_kernel<64>, grid, block, st, a, parts, n_real);
+hipError_t launch_attn_few(const FwdArgs& a, const ItemList& list, int D, int n_real, hipStream_t st) {
+  const dim3 parts(a.n_items * a.parts), rows(a.T_q, a.H);
+  const hipError_t e =
+      D == 128 ? sp_launch(kKFwd, attn_fwd_kernel<128, false, 4, false, true, true>, parts, dim3(NT), st, a, list)
+               : sp_launch(kKFwd, attn_fwd_kernel<64, false, 4, false, true, true>, parts, dim3(NT), st, a, list);
+  if (e != hipSuccess) return e;
+  return D == 128 ? sp_launch(0, attn_join_kernel<128>, rows, dim3(kJoinThreads), st, a, n_real)
+                  : sp_launch(0, attn_join_kernel<64>, rows, dim3(kJoinThreads), st, a, n_real);
 }
 
 template <int D, int KW, bool TWO>

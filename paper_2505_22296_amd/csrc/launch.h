@@ -139,9 +139,6 @@ struct ReduceArgs {
 //   fwd / dq of a batch with shared prefixes:
 //              {record, 0, 0, 0, 0, head, kv_head, 0}: the record of the item's
 //              first workgroup, in ints from the list's start (layout: RowSlot)
-//   fwd of few rows, shared prefixes:
-//              {record, part, windows, query heads a slot, 0, head, kv_head, 0}: windows,
-//              the place of {own key begin, end} of every row
 //   zero fill of a dummy query slot (fwd / dq): {r_begin, r_end, 0, 0, 0, slot, 0, 2}
 //   zero fill of a KV head no real query head reads (dk/dv):
 //              {k_begin, k_end, 0, 0, 0, 0, kv_head, 3}
@@ -176,6 +173,7 @@ struct FwdArgs {
   float scale_log2;    // softmax_scale * log2(e)
   int causal, init;
   int n_items;
+  int parts;           // few rows: of every tile's keys
 };
 
 struct DqArgs {
@@ -263,11 +261,21 @@ struct LaunchShape {
 // `prefix`: the row items name records (shared prefixes); not with `merge`.
 hipError_t launch_attn_fwd(const FwdArgs& a, const ItemList& list, LaunchShape s, int D, bool merge, bool prefix,
                            hipStream_t st);
-// A shared-prefix forward of few rows: every item one workgroup with a part of the
-// keys, then the merge of the parts (partial results in o_acc, lse_acc: [parts, T_q,
-// H, D], [parts, H, T_q]).
+// A shared-prefix forward of few rows, in tiles of two slots (a work item's place in
+// the launch's list each, behind them {own key begin, end} of every row): rows
+// [row0, row1) of `heads` query heads from `head` on see keys [p0, p1) of their prefix
+// and own windows inside [k0, k1).
+struct FewTile {
+  int32_t row0, row1, p0, p1, k0, k1, head_heads, kv;  // head | heads << 16
+};
+static_assert(sizeof(FewTile) == kItemInts * sizeof(int32_t), "a tile takes an item's place");
+static constexpr int few_steps(int k0, int k1, int tile_keys) {  // key tiles of keys [k0, k1)
+  return k1 > k0 ? (k1 - (k0 & ~7) + tile_keys - 1) / tile_keys : 0;
+}
+// Then the merge of the parts (partial results in o_acc, lse_acc: [parts, T_q, H, D],
+// [parts, H, T_q]).
 static constexpr int kMaxParts = 256;
-hipError_t launch_attn_few(const FwdArgs& a, const ItemList& list, int D, int parts, int n_real, hipStream_t st);
+hipError_t launch_attn_few(const FwdArgs& a, const ItemList& list, int D, int n_real, hipStream_t st);
 hipError_t launch_attn_dq(const DqArgs& a, const ItemList& list, LaunchShape s, int D, bool prefix, hipStream_t st);
 hipError_t launch_attn_dkdv(const DkdvArgs& a, const ItemList& list, LaunchShape s, int D, hipStream_t st);
 // dQ and dK/dV in one launch; (q.split, k.split) one of (4, 2), (2, 1),

@@ -279,3 +279,51 @@ def test_policy_sums_feed_the_loss_reduction(sp):
         dl = sp.sp_policy_loss_bwd(p, x["x"], x["labels"], *o[:3], x["old"], x["ref"], x["adv"], cu, grad[i].contiguous())
         big = w["dx"].abs().amax(1, keepdim=True)
         check("dlogits", dl, w["dx"], STEP16 * w["dx"].abs() + 64 * (tol + EPS32 * 64) * big + 2.0 ** -126)
+
+
+def test_policy_labels_that_do_not_count(sp):
+    """Labels outside [0, V), an ignored label inside it, tokens outside the
+    sequences: zero, and their logits are not looked at."""
+    T, V, cu = 12, 64, [1, 6, 11]
+    d = make(T, V, cu, seed=21, ignored=0.0)
+    d["labels"][2], d["labels"][3], d["labels"][7], d["labels"][8] = V, -1, 2 ** 31 - 1, -2 ** 31
+    d["labels"][4] = d["labels"][9] = 5  # the ignored one here
+    x = device(d)
+    out = [0, 2, 3, 4, 7, 8, 9, 11]
+    x["x"][out] = math.nan
+    p = sp.PolicyParams(0.2, 0.3, 0.1, 0.01, ignore_index=5)
+    logp, lse, ent, sums, stats = sp.sp_policy_loss(p, x["x"], x["labels"], x["old"], x["ref"], x["adv"], cu)
+    dl = sp.sp_policy_loss_bwd(p, x["x"], x["labels"], logp, lse, ent, x["old"], x["ref"], x["adv"], cu, x["grad"])
+    keep = [i for i in range(T) if i not in out]
+    for t in (logp, lse, ent, dl):
+        assert not t[out].any() and torch.isfinite(t).all() and t[keep].any()
+    d["labels"][out] = -100
+    d["x"][out] = 0.0
+    want = reference(d, 0.1, 0.01)
+    assert stats[:, 3].tolist() == [2.0, 2.0]
+    tol = lse_tol(d, want["lse"])
+    check("seq_sum", sums, want["sums"], 4 * tol.max() * want["size"])
+
+
+def test_policy_offsets_past_32_bits(sp):
+    """The last rows of 15000 x 152064 logits (2.3e9 of them): the same bits as in a
+    call of their own."""
+    T, V, n = 15000, 152064, 40
+    x = torch.zeros(T, V, dtype=torch.bfloat16, device="cuda")
+    g = torch.Generator(device="cuda").manual_seed(3)
+    x[-n:] = torch.randn(n, V, generator=g, device="cuda").bfloat16()
+    lab = torch.full((T,), -100, dtype=torch.int32, device="cuda")
+    lab[-n:] = torch.randint(0, V, (n,), generator=g, device="cuda", dtype=torch.int32)
+    f = [torch.randn(T, generator=g, device="cuda") - 12 for _ in range(2)]
+    adv, up = torch.ones(1, device="cuda"), torch.ones(1, device="cuda")
+    p = sp.PolicyParams(0.2, 0.3, 0.1, 0.01)
+    tail = slice(T - n, T)
+    # (a row of the small call is summed in more parts: its logp differs by roundings)
+    out = sp.sp_policy_loss(p, x, lab, *f, adv, [0, T])
+    few = sp.sp_policy_loss(p, x[tail], lab[tail], f[0][tail], f[1][tail], adv, [0, n])
+    assert (out[0][tail] - few[0]).abs().max() <= 64 * EPS32 * 16 and not out[0][:-n].any()
+    own = [t[tail].contiguous() for t in out[:3]]
+    want = sp.sp_policy_loss_bwd(p, x[tail], lab[tail], *own, f[0][tail], f[1][tail], adv, [0, n], up)
+    dl = sp.sp_policy_loss_bwd(p, x, lab, *out[:3], *f, adv, [0, T], up, dlogits=x)
+    assert torch.equal(dl[tail], want) and want.any()
+    assert not dl[:-n].any()

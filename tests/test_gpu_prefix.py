@@ -247,3 +247,62 @@ def test_prefix_dq_accumulator_and_gradients_over_inputs(sp):
     sp.sp_attn_bwd(d, q, k2, v2, o, lse, do, dq_acc=acc, dk=k2, dv=v2)
     assert torch.equal(k2, dk) and torch.equal(v2, dv)
     assert torch.equal((acc - 1).bfloat16(), dq) or ((acc - 1) - dq.float()).abs().max() <= STEP16 * dq.abs().max() + 1e-6
+
+
+def test_prefix_on_a_rank_of_dummy_slots_and_empty_inputs(sp):
+    """No real query head, no rows, no keys."""
+    cu = np.array([0, 40, 60], np.int32)
+    kw = dict(head_dim=64, H_loc=1, head_offset=3, num_real_heads=3, num_padded_heads=4, gqa_group=1, Hkv_loc=1,
+              kv_head_offset=3, prefix_of=[-1, 0])
+    d = sp.Desc(T_q=60, T_k=60, cu_seqlens_q=cu, cu_seqlens_k=cu, **kw)
+    q, k, v, do = inputs(d, 1)
+    o, lse = sp.sp_attn_fwd(d, q, k, v)
+    grads = sp.sp_attn_bwd(d, q, k, v, o, lse, do)
+    assert not any(t.view(torch.int16).any() for t in (o, *grads)) and (lse == -math.inf).all()
+    zero = np.zeros(3, np.int32)
+    d = sp.Desc(T_q=0, T_k=60, cu_seqlens_q=zero, cu_seqlens_k=cu, **dict(kw, head_offset=0, kv_head_offset=0))
+    q, k, v, do = inputs(d, 1)
+    o, lse = sp.sp_attn_fwd(d, q, k, v)
+    dq, dk, dv = sp.sp_attn_bwd(d, q, k, v, o, lse, do)
+    assert not dk.view(torch.int16).any() and not dv.view(torch.int16).any()
+    d = sp.Desc(T_q=60, T_k=0, cu_seqlens_q=cu, cu_seqlens_k=zero, causal=False,
+                **dict(kw, head_offset=0, kv_head_offset=0))
+    q, k, v, do = inputs(d, 1)
+    o, lse = sp.sp_attn_fwd(d, q, k, v)
+    dq, _, _ = sp.sp_attn_bwd(d, q, k, v, o, lse, do)
+    assert not o.view(torch.int16).any() and not dq.view(torch.int16).any() and (lse == -math.inf).all()
+
+
+def test_prefix_row_statistics_are_kept(sp):
+    """A second backward on the same workspace with SP_DESC_ROWSTATS_READY."""
+    nq, pre = [260, 90, 70], [-1, 0, 0]
+    d, p = desc(nq, nq, pre, D=128, hq=4, hkv=1)
+    q, k, v, do = inputs(d, 4)
+    o, lse = sp.sp_attn_fwd(d, q, k, v)
+    ws = torch.empty(sp.sp_attn_workspace_size(d, sp.SP_OP_BWD), dtype=torch.uint8, device="cuda")
+    want = sp.sp_attn_bwd(d, q, k, v, o, lse, do, workspace=ws)
+    d.c.flags |= sp.SP_DESC_ROWSTATS_READY
+    got = sp.sp_attn_bwd(d, q, k, v, o, lse, do, workspace=ws)
+    assert all(torch.equal(a, b) for a, b in zip(want, got))
+
+
+def test_prefix_offsets_past_32_bits(sp):
+    """A group at the end of 2.1 million keys of 8 heads (2.2e9 elements a tensor), whose
+    other keys no row sees: the bits of the group alone, and no gradient before it."""
+    n, H, D = 2100000, 8, 128
+    for nq, nk in (([300, 120, 40], [300, 120, 40]), ([0, 1, 1], [9000, 40, 1])):
+        d, _ = desc([0] + nq, [n] + nk, [-1, -1, 1, 1], D=D, hq=H, hkv=H)
+        e, _ = desc(nq, nk, [-1, 0, 0], D=D, hq=H, hkv=H)
+        q, k, v, do = inputs(e, 6)
+        K, V = (torch.zeros(d.c.T_k, H, D, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+        K[n:], V[n:] = k, v
+        assert list(sp.sp_attn_plan(d, sp.SP_OP_FWD).values()) == list(sp.sp_attn_plan(e, sp.SP_OP_FWD).values())
+        o, lse = sp.sp_attn_fwd(d, q, K, V)
+        o2, l2 = sp.sp_attn_fwd(e, q, k, v)
+        assert torch.equal(o, o2) and torch.equal(lse, l2)
+        dq, dk, dv = sp.sp_attn_bwd(d, q, K, V, o, lse, do, dk=K, dv=V)
+        dq2, dk2, dv2 = sp.sp_attn_bwd(e, q, k, v, o, lse, do)
+        for a, b in ((dq, dq2), (dk[n:], dk2), (dv[n:], dv2)):  # (another plan sums in another order)
+            assert (a.float() - b.float()).abs().max() <= 8 * STEP16 * b.float().abs().max()
+        assert not dk[:n].any() and not dv[:n].any()
+        del K, V, dk, dv

@@ -63,6 +63,8 @@ CASES = [  # T, D, Hq, Hkv, sp, maps, rot, neighbours, norm, positions
     (40, 64, 7, 7, 2, MHA7, 0, False, True, "ramp"),
     (5000, 64, 2, 1, 1, ([0, 1], [0]), 64, False, True, "ramp"),  # more tokens than the backward has wavefronts
     (17, 128, 3, 2, 1, ([2, 0, 2], [-1, 1]), 16, False, True, "none"),  # heads twice, and in no slot
+    (9, 64, 100, 70, 4, (list(range(100)) + [-1] * 4, list(range(70)) + [3, -1]), 64, False, True, "ramp"),  # large maps
+    (20, 64, 2, 2, 2, ([-1, 0, -1, 1], [1, -1, -1, -1]), 48, True, True, "ramp"),  # slots without heads first
 ]
 
 
@@ -280,3 +282,24 @@ def test_qk_in_a_graph(sp):
     on_side = step(sets[1], stream=side)
     side.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(on_side, eager[1]))
+
+
+def test_qk_offsets_past_32_bits(sp):
+    """Tokens 8192 elements apart whose last one lies past 2^31 elements."""
+    T, D, n = 263000, 64, 50
+    buf = torch.empty(T, 8192, dtype=torch.bfloat16, device="cuda")
+    rows = torch.randn(T, 3, D, device="cuda").bfloat16()
+    buf[:, :192] = rows.view(T, 192)
+    q, k, v = (buf[:, i * D:(i + 1) * D].view(T, 1, D) for i in range(3))
+    w = torch.randn(2, D, device="cuda").bfloat16()
+    kw = dict(head_dim=D, H_q=1, H_kv=1, sp=1, q_map=[0], kv_map=[0], inv_freq=freqs(D))
+    far = sp.sp_qk_norm_rope(sp.QkDesc(T=T, **kw), q, k, v, None, w[0], w[1])
+    near = sp.sp_qk_norm_rope(sp.QkDesc(T=n, position_base=T - n, **kw),
+                              *(rows[T - n:, i:i + 1].contiguous() for i in range(3)), None, w[0], w[1])
+    assert all(torch.equal(a[:, T - n:], b) for a, b in zip(far, near))
+    up = [torch.randn(1, T, 1, D, device="cuda").bfloat16() for _ in range(3)]
+    want = sp.sp_qk_norm_rope_bwd(sp.QkDesc(T=n, position_base=T - n, **kw), rows[T - n:, :1].contiguous(),
+                                  rows[T - n:, 1:2].contiguous(), *(u[:, T - n:].contiguous() for u in up), None, w[0], w[1])
+    got = sp.sp_qk_norm_rope_bwd(sp.QkDesc(T=T, **kw), q, k, *up, None, w[0], w[1], dq=q, dk=k, dv=v)
+    assert all(torch.equal(a[T - n:], b) for a, b in zip(got[:3], want[:3]))
+    assert not torch.isnan(got[3]).any()

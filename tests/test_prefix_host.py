@@ -150,6 +150,31 @@ def test_lists_cover_exactly_the_mask(data):
     check_lists(d, p, hq)
 
 
+def test_plans_of_calls_without_rows_heads_or_keys():
+    """Sizes and plans of shared-prefix calls with nothing to do."""
+    for nq, nk in (([0, 0], [50, 3]), ([50, 3], [0, 0]), ([0, 0], [0, 0])):
+        d, _ = desc(nq, nk, [-1, 0], causal=False)
+        for op in (sp.SP_OP_FWD, sp.SP_OP_BWD):
+            assert status(d, op) == sp.SP_OK
+            assert len(sp.sp_attn_plan(d, op)) == 6
+    d = sp.Desc(T_q=8, T_k=8, head_dim=64, H_loc=1, head_offset=3, num_real_heads=3, num_padded_heads=4, gqa_group=1,
+                Hkv_loc=1, kv_head_offset=3, cu_seqlens_q=[0, 4, 8], cu_seqlens_k=[0, 4, 8], prefix_of=[-1, 0])
+    assert status(d) == sp.SP_OK and sp.sp_attn_plan(d, sp.SP_OP_FWD)["key_split"] == 0
+    assert len(sp.sp_attn_schedule(d, sp.SP_OP_FWD)) == 0
+
+
+def test_few_rows_take_parts_of_the_keys():
+    """Many keys and few rows; not where the rows alone fill the launch, or their
+    windows do not fit its arguments."""
+    for nq, nk, split in (([0, 1, 1], [20000, 30, 40], True), ([0, 1, 1], [300, 30, 40], False),
+                          ([2000, 40, 40], [2000, 40, 40], False), ([0, 2100], [20000, 2100], False)):
+        d, _ = desc(nq, nk, [-1] + [0] * (len(nq) - 1))
+        parts = sp.sp_attn_plan(d, sp.SP_OP_FWD)["key_split"]
+        assert (parts >= 2) == split and parts <= 256
+        small = sp.sp_attn_workspace_size(d, sp.SP_OP_FWD)
+        assert small >= parts * d.c.T_q * d.c.H_loc * (d.c.head_dim + 1) * 4
+
+
 def test_rests_of_answers_share_tiles():
     """Sixteen answers of 600 rows to a prompt: 2 full tiles an answer, and 88 rows
     left, three groups of rows, of all answers in 6 tiles; the prompt has 3."""
