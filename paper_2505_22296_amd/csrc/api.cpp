@@ -648,14 +648,6 @@ Costs schedule_row_items(const sp_attn_desc* d, const Problem& p, const std::vec
   return p.prefix.empty() ? schedule_rows(d, p, BM, BN, include_empty, out, n_front)
                           : schedule_tiles(d, p, tiles, BN, out, n_front, items);
 }
-// The model's time of a shared-prefix forward without parts.
-double whole_us(const sp_attn_desc* d, const Problem& p) {
-  std::vector<int32_t> v;
-  std::vector<Item> rows;
-  double us = 0;
-  choose_shape(schedule_tiles(d, p, row_tiles(d, p), spk::kFwdBN, v, 0, rows), kSplitFwd, p.D, us);
-  return us;
-}
 // Ints of the records under any split.
 size_t record_room(size_t n_tiles) { return n_tiles * 4 * (size_t)spk::record_ints(kSlots / 4); }
 
@@ -711,26 +703,15 @@ std::vector<int32_t> merged_items(const std::vector<Item>& rows, const std::vect
 constexpr double kFewStageUs = 1.6, kFewJoinUs = 8, kFewBytesUs = 2e6;
 constexpr int kFewSlots = 2, kFewSplit = kSlots / kFewSlots;
 struct FewPlan {
-  int parts = 0;  // 0: not taken
+  int parts = 0;  // 0: not possible
+  double us = 0;  // the model's time
   std::vector<spk::FewTile> tiles;
-  std::vector<int32_t> windows;  // own keys [begin, end) of every row
 };
-// `whole_us`: the model's time of the launch without parts.
-FewPlan few_plan(const sp_attn_desc* d, const Problem& p, double whole_us) {
+FewPlan few_plan(const sp_attn_desc* d, const Problem& p) {
   constexpr size_t kInts = std::size(decltype(spk::ItemList::v){});
   FewPlan f;
   if (p.prefix.empty() || p.n_real == 0 || d->T_q == 0 || (size_t)2 * d->T_q > kInts) return f;
-  std::vector<int> prefix(d->T_q, -1);
-  f.windows.assign((size_t)2 * d->T_q, 0);
-  for (size_t s = 0; s < p.segs.size(); ++s) {
-    const Seg& g = p.segs[s];
-    for (int i = g.qa; i < g.qb; ++i) {
-      prefix[i] = p.prefix[s];
-      const int k1 = d->causal ? (int)std::min<int64_t>(g.kb, (int64_t)i + g.delta + 1) : g.kb;
-      f.windows[2 * i] = g.ka;
-      f.windows[2 * i + 1] = std::max(g.ka, k1);
-    }
-  }
+  if ((int64_t)d->T_q * p.n_real > (int64_t)kCus / 2 * kFewSlots * kSlotRows) return f;
   int longest = 0;
   const int BN = spk::fwd_tile_keys(p.D, kFewSplit);
   for (int kv = 0; kv < d->Hkv_loc; ++kv) {
@@ -738,34 +719,58 @@ FewPlan few_plan(const sp_attn_desc* d, const Problem& p, double whole_us) {
     for (int b = 0; b < blocks; ++b) {
       const int h0 = p.kv_lo[kv] + n * b / blocks, heads = p.kv_lo[kv] + n * (b + 1) / blocks - h0;
       const int rows = kFewSlots * (kSlotRows / heads);
-      for (int i = 0; i < d->T_q;) {
-        int e = i + 1;
-        while (e < d->T_q && e < i + rows && prefix[e] == prefix[i]) ++e;
-        spk::FewTile t{i, e, 0, 0, 0, 0, h0 | heads << 16, kv};
-        if (prefix[i] >= 0) {
-          t.p0 = p.segs[prefix[i]].ka;
-          t.p1 = p.segs[prefix[i]].kb;
+      // rows of one prefix after the other, segment by segment (then those behind
+      // the last segment, which see nothing)
+      spk::FewTile t{0, 0, 0, 0, 0, 0, h0 | heads << 16, kv};
+      int of = -1;
+      auto flush = [&] {
+        if (t.row1 > t.row0) {
+          longest = std::max(longest, spk::few_steps(t.p0, t.p1, BN) + spk::few_steps(t.k0, t.k1, BN));
+          f.tiles.push_back(t);
         }
-        for (int r = i; r < e; ++r) {
-          const int a = f.windows[2 * r], z = f.windows[2 * r + 1];
-          if (z <= a) continue;
-          t.k0 = t.k1 > t.k0 ? std::min(t.k0, a) : a;
-          t.k1 = std::max(t.k1, z);
+        t.row0 = t.row1;
+        t.k0 = t.k1 = 0;
+      };
+      auto add = [&](const Seg& g, int prefix) {
+        if (g.qb <= g.qa) return;
+        if (prefix != of) flush();
+        of = prefix;
+        t.p0 = prefix >= 0 ? p.segs[prefix].ka : 0;
+        t.p1 = prefix >= 0 ? p.segs[prefix].kb : 0;
+        for (int a = g.qa; a < g.qb; a = t.row1) {
+          if (t.row1 - t.row0 == rows) flush();
+          t.row1 = std::min(g.qb, t.row0 + rows);
+          const int k1 = d->causal ? (int)std::min<int64_t>(g.kb, (int64_t)t.row1 + g.delta) : g.kb;
+          if (k1 <= g.ka) continue;
+          t.k0 = t.k1 > t.k0 ? std::min(t.k0, g.ka) : g.ka;
+          t.k1 = std::max(t.k1, k1);
         }
-        longest = std::max(longest, spk::few_steps(t.p0, t.p1, BN) + spk::few_steps(t.k0, t.k1, BN));
-        f.tiles.push_back(t);
-        i = e;
-      }
+      };
+      for (size_t s = 0; s < p.segs.size(); ++s) add(p.segs[s], p.prefix[s]);
+      add(Seg{p.q_pad, d->T_q, 0, 0, 0}, -1);
+      flush();
+      if (f.tiles.size() * 2 > kCus || f.tiles.size() * kItemInts + 2 * d->T_q > kInts) return f;
     }
   }
-  if (f.tiles.size() * kItemInts + f.windows.size() > kInts) return f;
   const int stages = (longest + kFewSplit - 1) / kFewSplit;  // of four tiles
   const int parts = (int)std::min<size_t>({kCus / f.tiles.size(), (size_t)stages / 2, (size_t)spk::kMaxParts});
   if (parts < 2) return f;
-  const double us = kStartUs + (double)((stages + parts - 1) / parts) * kFewStageUs + kFewJoinUs +
-                    2.0 * parts * d->T_q * d->H_loc * p.D * 4 / kFewBytesUs;
-  if (us < 0.8 * whole_us) f.parts = parts;
+  f.parts = parts;
+  f.us = kStartUs + (double)((stages + parts - 1) / parts) * kFewStageUs + kFewJoinUs +
+         2.0 * parts * d->T_q * d->H_loc * p.D * 4 / kFewBytesUs;
   return f;
+}
+// Whether it is taken; `whole_us`: the model's time of the launch without parts.
+bool few_taken(const FewPlan& f, double whole_us) { return f.parts > 0 && f.us < 0.8 * whole_us; }
+// Own keys [begin, end) of every row.
+void few_windows(const sp_attn_desc* d, const Problem& p, int32_t* out) {
+  std::fill(out, out + (size_t)2 * d->T_q, 0);
+  for (const Seg& g : p.segs)
+    for (int i = g.qa; i < g.qb; ++i) {
+      const int k1 = d->causal ? (int)std::min<int64_t>(g.kb, (int64_t)i + g.delta + 1) : g.kb;
+      out[2 * i] = g.ka;
+      out[2 * i + 1] = std::max(g.ka, k1);
+    }
 }
 
 // Zero fills as work items of the same launch (no extra kernels): dummy
@@ -1280,9 +1285,9 @@ sp_status sp_attn_workspace_size(const sp_attn_desc* desc, int32_t op, size_t* b
   size_t a = 0, b = 0;
   item_counts(desc, p, op, a, b);
   *bytes = layout_for(desc, p, op, a, b).total;
-  if (op == SP_OP_FWD && !p.prefix.empty()) {
-    const FewPlan f = few_plan(desc, p, whole_us(desc, p));
-    if (f.parts) *bytes = layout_few(desc, p, f).total;
+  if (op == SP_OP_FWD) {  // (either way of a shared-prefix forward fits)
+    const FewPlan f = few_plan(desc, p);
+    if (f.parts) *bytes = std::max(*bytes, layout_few(desc, p, f).total);
   }
   return SP_OK;
 }
@@ -1344,7 +1349,8 @@ sp_status sp_attn_plan(const sp_attn_desc* desc, int32_t op, int32_t* plan) {
     double us;
     b.q = choose_shape(schedule_row_items(desc, p, tiles, spk::kFwdBM, spk::kFwdBN, true, v, 0, rows), kSplitFwd,
                        p.D, us);
-    b.k.split = few_plan(desc, p, us).parts;
+    const FewPlan few = few_plan(desc, p);
+    if (few_taken(few, us)) b.k.split = few.parts;
   }
   const int32_t r[SP_PLAN_INTS] = {b.q.split, b.q.two, b.k.split, b.k.two, b.one, b.dq_first};
   std::copy(r, r + SP_PLAN_INTS, plan);
@@ -1409,7 +1415,7 @@ static sp_status fwd_few(const sp_attn_desc* d, const Problem& p, const FewPlan&
   spk::FwdArgs a{};
   spk::ItemList list{};
   std::memcpy(list.v, few.tiles.data(), few.tiles.size() * sizeof(spk::FewTile));
-  std::copy(few.windows.begin(), few.windows.end(), list.v + few.tiles.size() * kItemInts);
+  few_windows(d, p, list.v + few.tiles.size() * kItemInts);
   a.q = (const uint16_t*)q; a.k = (const uint16_t*)k; a.v = (const uint16_t*)v;
   a.o = (uint16_t*)o; a.lse = lse;
   a.o_acc = (float*)at(ws, L.few_o); a.lse_acc = (float*)at(ws, L.few_lse);
@@ -1454,8 +1460,8 @@ static sp_status fwd_common(const sp_attn_desc* d, const void* q, const void* k,
   double us;
   const spk::LaunchShape shape = choose_shape(cost, kSplitFwd, p.D, us);
   if (prefix && !static_ws) {
-    const FewPlan few = few_plan(d, p, us);
-    if (few.parts) return fwd_few(d, p, few, q, k, v, o, lse, ws, ws_bytes, (hipStream_t)stream);
+    const FewPlan few = few_plan(d, p);
+    if (few_taken(few, us)) return fwd_few(d, p, few, q, k, v, o, lse, ws, ws_bytes, (hipStream_t)stream);
   }
   if (prefix) {
     const std::vector<int32_t> records =
