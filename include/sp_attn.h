@@ -509,7 +509,8 @@ sp_status sp_loss_reduce(const float* partial_sums, const float* ref_partial_sum
  * sums over tokens in float64 in a fixed order: repeating a call gives the same
  * bits.  A logit of -inf has probability 0; a row of nothing above -6.9e29 has lse
  * = logp = -inf and entropy 0; +inf or NaN in a counted row make the token's values
- * NaN.  r A counts as 0 where A is 0.
+ * NaN.  r A counts as 0 where A is 0, a difference of log-probabilities where both
+ * are -inf, and the kl of a row with lse = -inf; may be captured into a graph.
  *
  * logits: DEVICE bf16 [T, V] row-major, 16-byte aligned, V a multiple of 8; labels:
  * DEVICE int32 [T]; old_logp, ref_logp: DEVICE float32 [T], ref_logp may be NULL

@@ -88,6 +88,12 @@ SP_DEV bool label_counts(const LossArgs& a, int label) {
   return label != a.ignore_index && label >= 0 && label < a.V;
 }
 
+// a - b of log-probabilities; 0 where both are -inf (a banned token is banned in both).
+template <typename T>
+SP_DEV T log_ratio(T a, T b) {
+  return a == b ? (T)0 : a - b;
+}
+
 // What a token contributes, in 64 bits from the sums of its row: a thread does
 // it once a row, and e^d - d - 1 of a small d keeps its digits.
 struct TokenTerms {
@@ -110,7 +116,7 @@ SP_DEV TokenTerms token_terms(const PolicyArgs& p, const RowSum& r, uint16_t lab
   } else {
     lse = lp = ent = __builtin_nan("");
   }
-  const double ratio = exp(lp - (double)tok.old_logp[t]);
+  const double ratio = exp(log_ratio(lp, (double)tok.old_logp[t]));
   const double held = fmin(fmax(ratio, 1.0 - (double)p.clip_low), 1.0 + (double)p.clip_high);
   // (an advantage of zero beside an infinite ratio is zero)
   const double free_obj = adv == 0.f ? 0.0 : ratio * (double)adv, held_obj = held * (double)adv;
@@ -118,8 +124,9 @@ SP_DEV TokenTerms token_terms(const PolicyArgs& p, const RowSum& r, uint16_t lab
   o.term = -(free_obj > held_obj ? held_obj : free_obj);
   o.kl = 0.0;
   if (p.has_ref) {
-    const double d = (double)tok.ref_logp[t] - lp;
-    o.kl = expm1(d) - d;
+    // (a row without a distribution diverges from none; a label banned here alone, infinitely)
+    const double d = r.s == 0.f ? 0.0 : log_ratio((double)tok.ref_logp[t], lp);
+    o.kl = d < __builtin_inf() ? expm1(d) - d : d;
     if (p.kl_coef != 0.f) o.term += (double)p.kl_coef * o.kl;
   }
   if (p.entropy) o.term -= (double)p.entropy_coef * ent;
@@ -280,10 +287,10 @@ __global__ __launch_bounds__(kPB) void policy_bwd_kernel(LossArgs a, PolicyArgs 
   for (int i = 0; i < kPU; ++i)
     if (c0 + i * kPB < nch) v[i] = ld_stream(&logits[base + c0 + i * kPB]);
   const float G = grad_seq[s], A = tok.adv[p.adv_per_token ? t : s], lp = tok.logp[t];
-  const float ratio = expf(lp - tok.old_logp[t]);
+  const float ratio = expf(log_ratio(lp, tok.old_logp[t]));
   const bool free_side = A >= 0.f ? ratio <= 1.f + p.clip_high : ratio >= 1.f - p.clip_low;
   float g = free_side && A != 0.f ? -A * ratio : 0.f;
-  if (p.has_ref && p.kl_coef != 0.f) g -= p.kl_coef * expm1f(tok.ref_logp[t] - lp);
+  if (p.has_ref && p.kl_coef != 0.f) g -= p.kl_coef * expm1f(log_ratio(tok.ref_logp[t], lp));
   g *= G;
   const float lb = l * kLog2e;
   // dx = 2^y (k1 y + k0) with y = log2 p: the entropy's part is G c_ent p (y ln 2 + H)

@@ -327,3 +327,30 @@ def test_policy_offsets_past_32_bits(sp):
     dl = sp.sp_policy_loss_bwd(p, x, lab, *out[:3], *f, adv, [0, T], up, dlogits=x)
     assert torch.equal(dl[tail], want) and want.any()
     assert not dl[:-n].any()
+
+
+def test_policy_kl_of_banned_labels(sp):
+    """A label of probability 0, and rows without a distribution, beside a reference
+    model: finite wherever both models ban the token, and infinite where one does."""
+    T, V, cu = 6, 1000, [0, 3, 4, 6]
+    d = make(T, V, cu, seed=21, ignored=0.0)
+    d["x"][0] = -math.inf                    # no distribution, a finite reference
+    for t in (1, 3):
+        d["x"][t, d["labels"][t]] = -math.inf  # the label alone
+    d["x"][2] = -math.inf
+    d["ref"][1:3] = d["old"][2] = -math.inf    # banned in all models
+    d["adv"][:] = 1.0
+    x = device(d)
+    p = sp.PolicyParams(0.2, 0.3, 0.5)
+    logp, lse, _, sums, stats = sp.sp_policy_loss(p, x["x"], x["labels"], x["old"], x["ref"], x["adv"], cu,
+                                                  with_entropy=False)
+    assert (logp[:4] == -math.inf).all() and torch.isfinite(lse[[1, 3]]).all()
+    # ratios 0, 0 and 1 (nothing differs), no divergence: -(0 + 0 + 1)
+    assert sums[0] == -1.0 and stats[0].tolist() == [0.0, 0.0, 0.0, 3.0]
+    assert sums[1] == math.inf and stats[1][0] == math.inf
+    want = reference({k: v[4:] if k in ("x", "labels", "old", "ref") else v for k, v in
+                      dict(d, adv=d["adv"][2:], grad=d["grad"][2:], cu=[0, 2]).items()}, kl=0.5, ent_coef=0.0)
+    tol = lse_tol(d, want["lse"]).max() * (2 * want["size"] + 2)
+    check("sums", sums[2:], want["sums"], tol)
+    dl = sp.sp_policy_loss_bwd(p, x["x"], x["labels"], logp, lse, None, x["old"], x["ref"], x["adv"], cu, x["grad"])
+    assert not dl[:3].any() and torch.isfinite(dl[4:]).all() and dl[4:].any()
