@@ -25,9 +25,9 @@
 // depends on the token -- the angles -- is formed once for the whole range, and the
 // next head's loads are in flight while one is worked on.  (Heads on the lanes and
 // one token a wavefront instead: forward of 4096 tokens of 28 / 4 heads to 8 ranks,
-// D = 128, 20.1 us, now 17.8, 5.9 TB/s; their backward, with the sum of the weight
-// gradients, 53 us, now 33; of 8191 tokens of 40 / 8 heads from 16 ranks 104 us, now
-// 76, 5.0 TB/s.)
+// D = 128, 20.1 us, now 17.7, 5.9 TB/s; their backward, with the sum of the weight
+// gradients, 53 us, now 31, 3.9 TB/s; of 8191 tokens of 40 / 8 heads from 16 ranks 104
+// us, now 76 to 81, 4.9 TB/s.)
 #include <algorithm>
 #include <type_traits>
 
