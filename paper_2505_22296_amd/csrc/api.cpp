@@ -700,7 +700,7 @@ std::vector<int32_t> merged_items(const std::vector<Item>& rows, const std::vect
 // windows fit the launch's own list: a copy of them would take longer than it gains
 // (a prompt of 1689 rows and 13 answers of 39, copied, 37 us, in whole walks 23).  16
 // answers of one row to 32768 keys, 7 heads: 308 -> 21 us; 64 answers to 8192 keys, 4
-// heads, 78 -> 17.  (Over 40 drawn sizes with parts 0.85 to 8.9 times as fast, 1.9 at the
+// heads, 78 -> 17.  (Over 40 drawn sizes with parts 0.85 to 8.9 times as fast, 2.1 at the
 // median; the losses are single calls of 12 to 16 us.)
 constexpr double kFewStageUs = 1.6, kFewJoinUs = 8, kFewBytesUs = 2e6;
 constexpr int kFewSlots = 2, kFewSplit = kSlots / kFewSlots;
