@@ -390,7 +390,8 @@ sp_status sp_f32_to_bf16(const float* src, void* dst, int64_t n, void* stream);
  *       first (its rows see the fewest keys).
  *       With SP_DESC_SHARED_PREFIX a row item holds up to eight groups of at most
  *       32 rows of segments that share a prefix; it is listed as one such entry a
- *       group, and one more with its prefix's keys and delta = 2^30.
+ *       group, and one more with its prefix's keys and delta = 2^30.  Key items of
+ *       a prefix are listed whole; a backward may cut their rows into parts.
  *   SP_OP_BWD, dK/dV items: {k_begin, k_end, q_begin, q_end, delta, head,
  *       kv_head, 1}.
  * A launch of few items splits each of them over S workgroups (row items: S =

@@ -323,6 +323,8 @@ struct SplitModel {
   double two;  // full CUs with two workgroups each against one (D = 64)
 };
 constexpr double kStartUs = 8;
+constexpr int kMaxKeyParts = 64, kKeyPartChunks = 8;  // key_cuts
+constexpr double kCutJoinUs = 10, kCutBytesUs = 4e6;
 constexpr size_t kCus = 256;
 constexpr SplitModel kSplitFwd{3, 2.0, {1.0, 1.22, 1.6}, 0.93};    // steps of 64 keys
 constexpr SplitModel kSplitDq{3, 1.03, {1.0, 1.15, 1.45}, 0.94};   // steps of 32 keys
@@ -651,17 +653,105 @@ Costs schedule_row_items(const sp_attn_desc* d, const Problem& p, const std::vec
 // Ints of the records under any split.
 size_t record_room(size_t n_tiles) { return n_tiles * 4 * (size_t)spk::record_ints(kSlots / 4); }
 
+// Shared prefixes whose key items are cut into parts of their rows, in the order of
+// the segments.  A short prompt's few key tiles see the rows of every answer: their
+// items would go on long after the others.  Parts are summed in float32 by one more
+// launch, in a fixed order.  The model: a backward takes the mean load of the CUs or its
+// longest item, under the best of plan_bwd's splits; a part adds a workgroup's start,
+// and its sums' way out and back; taken where that is 15% less or better.  Whole / in
+// parts, D = 128: 16 answers of 1000 rows to 512 keys, one head, 260 / 80 us; 32 of 1500
+// to 256, 4 heads, 876 / 446; 16 of 2000 to 512, 4 heads on one KV head, 569 / 468; 6 of
+// 361 to 144, one head, 47 / 29.  (Of 57 drawn batches it is taken in four, 0.96 to 1.57
+// times as fast.)
+std::vector<spk::KeyCut> key_cuts(const sp_attn_desc* d, const Problem& p) {
+  std::vector<spk::KeyCut> cuts;
+  if (p.prefix.empty() || p.n_real == 0) return cuts;
+  auto tiles = [](int n, int size) { return (double)((n + size - 1) / size); };
+  auto own = [&](const Seg& g) { return (g.qb - g.qa) * (d->causal ? 0.5 : 1.0); };  // of its rows, at the mean
+  double load_q = 0, load_k = 0, longest_q = 0, n_q = 0, n_k = 0;
+  for (size_t s = 0; s < p.segs.size(); ++s) {
+    const Seg& g = p.segs[s];
+    const double nq = tiles(g.qb - g.qa, spk::kDqBM), nk = tiles(g.kb - g.ka, spk::kDkdvBN);
+    const int prefix = p.prefix[s] < 0 ? 0 : p.segs[p.prefix[s]].kb - p.segs[p.prefix[s]].ka;
+    const double seen = prefix + (g.kb - g.ka) * (d->causal ? 0.5 : 1.0);
+    load_q += nq * seen / spk::kDqBN * kSplitDq.step;
+    if (nq > 0) longest_q = std::max(longest_q, (prefix + g.kb - g.ka) / (double)spk::kDqBN * kSplitDq.step);
+    const double rows = own(g) + p.segs_k[s].qb - g.qb;
+    load_k += nk * rows / spk::kDkdvBQ * kSplitDkdv.step;
+    n_q += nq * p.n_real;
+    n_k += nk * p.n_real;
+  }
+  const double step = p.D == 64 ? 0.7 : 1.0;  // (8 answers of 1000 rows, one head: 0.53 us a chunk, 0.76)
+  load_q *= step * p.n_real / kCus;
+  load_k *= step * p.n_real / kCus;
+  longest_q *= step;
+  // of a backward whose longest key item takes `us`, with `more` key items, under the
+  // splits that plan_bwd chooses from
+  const bool one = n_q + n_k <= kOneItems;
+  auto time = [&](double us, double more) {
+    constexpr int kPairs[3][2] = {{0, 0}, {1, 0}, {2, 1}};
+    double best = HUGE_VAL;
+    for (const auto& s : kPairs) {
+      const double rq = kSplitDq.rel[s[0]], rk = kSplitDkdv.rel[s[1]];
+      const double lq = load_q * rq + (n_q * (1 << s[0])) * kStartUs / kCus;
+      const double lk = load_k * rk + ((n_k + more) * (1 << s[1])) * kStartUs / kCus;
+      const double tq = longest_q * rq / (1 << s[0]) + kStartUs, tk = us * rk / (1 << s[1]) + kStartUs;
+      best = std::min(best, one ? std::max({lq + lk, tq, tk}) : std::max(lq, tq) + std::max(lk, tk));
+    }
+    return best;
+  };
+  int64_t row = 0;
+  for (size_t s = 0; s < p.segs.size() && cuts.size() < (size_t)spk::kMaxCuts; ++s) {
+    const Seg& g = p.segs_k[s];
+    if (g.qb == p.segs[s].qb || g.kb <= g.ka) continue;  // shared by none, or empty
+    const int len = g.kb - g.ka;
+    const int chunks = (g.qb - g.qa) / spk::kDkdvBQ;
+    const double longest = chunks * kSplitDkdv.step * step;
+    int best = 1;
+    double us = 0.85 * time(longest, 0);
+    for (int n = 2; n <= std::min(kMaxKeyParts, chunks / kKeyPartChunks); ++n) {
+      const double t = time(longest / n, tiles(len, spk::kDkdvBN) * p.n_real * (n - 1)) + kCutJoinUs +
+                       (double)len * n * p.n_real * p.D * 16 / kCutBytesUs;
+      if (t < us) {
+        us = t;
+        best = n;
+      }
+    }
+    const int64_t rows = (int64_t)len * best * p.n_real;
+    if (best == 1 || row + rows >= int64_t(1) << 28) continue;
+    cuts.push_back(spk::KeyCut{g.ka, len, best, (int)row});
+    row += rows;
+  }
+  return cuts;
+}
+int64_t cut_rows(const Problem& p, const std::vector<spk::KeyCut>& cuts) {
+  return cuts.empty() ? 0 : cuts.back().row + (int64_t)cuts.back().len * cuts.back().parts * p.n_real;
+}
+
 // Key-tile items (dK / dV).  Every key of every real head gets exactly one
-// item.  Leaves `items` longest first and returns their steps.
-Costs schedule_keys(const sp_attn_desc* d, const Problem& p, int BNK, int BQ,
+// item, or the parts of a cut.  Leaves `items` longest first and returns their steps.
+Costs schedule_keys(const sp_attn_desc* d, const Problem& p, int BNK, int BQ, const std::vector<spk::KeyCut>& cuts,
                     std::vector<int32_t>& out, size_t n_front, std::vector<Item>& items) {
   for (int y = 0; y < p.n_real; ++y) {
+    size_t next = 0;  // (cuts are in the order of the segments)
     for (const Seg& g : p.segs_k) {
+      const bool is_cut = next < cuts.size() && cuts[next].ka == g.ka && g.kb > g.ka;
+      const spk::KeyCut* cut = is_cut ? &cuts[next++] : nullptr;
       for (int a = g.ka; a < g.kb; a += BNK) {
         const int b = std::min(a + BNK, g.kb);
         int q0 = g.qa;
         if (d->causal) q0 = (int)std::max<int64_t>(g.qa, (int64_t)a - g.delta);
         const bool empty = q0 >= g.qb;
+        if (cut) {  // (parts without rows write zeros)
+          const int n = std::max(0, g.qb - q0), rows = ((n + cut->parts - 1) / cut->parts + BQ - 1) / BQ * BQ;
+          for (int i = 0; i < cut->parts; ++i) {
+            const int r0 = g.qb - std::min(n, i * rows), r1 = g.qb - std::min<int64_t>(n, (int64_t)(i + 1) * rows);
+            const int at = cut->row + (i * p.n_real + y) * cut->len + (a - g.ka);
+            items.push_back(Item{{a, b, r1, r0, g.delta, y, p.kv_of[y], 1 | (1 + at) << 2},
+                                 r1 < r0 ? ((r0 - (r1 & ~7)) + BQ - 1) / BQ : 0});
+          }
+          continue;
+        }
         Item it{{a, b, empty ? g.qb : q0, g.qb, g.delta, y, p.kv_of[y], 1}, 0};
         it.cost = empty ? 0 : (int64_t)((g.qb - (q0 & ~7)) + BQ - 1) / BQ;
         items.push_back(it);
@@ -819,12 +909,13 @@ int n_unread_kv(const sp_attn_desc* d, const Problem& p) {
 struct Layout {
   size_t items_dq = 0, items_kv = 0, neg_d = 0, lse2 = 0, part_k = 0, part_v = 0, total = 0;
   size_t few_o = 0, few_lse = 0;  // a forward of few rows
+  size_t cut_k = 0, cut_v = 0;    // parts of a backward's cut items
 };
 
 size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
 
 Layout layout_for(const sp_attn_desc* d, const Problem& p, int op, size_t n_items_a,
-                  size_t n_items_b) {
+                  size_t n_items_b, int64_t n_cut_rows = 0) {
   Layout L;
   size_t off = 0;
   auto take = [&](size_t bytes) {
@@ -847,6 +938,8 @@ Layout layout_for(const sp_attn_desc* d, const Problem& p, int op, size_t n_item
       L.part_k = take((size_t)p.n_real * d->T_k * D * 4);
       L.part_v = take((size_t)p.n_real * d->T_k * D * 4);
     }
+    L.cut_k = take((size_t)n_cut_rows * D * 4);
+    L.cut_v = take((size_t)n_cut_rows * D * 4);
   }
   L.total = std::max<size_t>(off, 256);
   return L;
@@ -876,8 +969,9 @@ size_t row_item_count(const sp_attn_desc* d, const Problem& p, int BM) {
   per_head += (size_t)((d->T_q - p.q_pad) + BM - 1) / BM;
   return per_head * (size_t)p.n_real + fills;
 }
-size_t key_item_count(const sp_attn_desc* d, const Problem& p, int BNK) {
+size_t key_item_count(const sp_attn_desc* d, const Problem& p, const std::vector<spk::KeyCut>& cuts, int BNK) {
   size_t per_head = 0;
+  for (const spk::KeyCut& c : cuts) per_head += (size_t)(c.parts - 1) * ((c.len + BNK - 1) / BNK);
   for (const Seg& g : p.segs_k) per_head += (size_t)((g.kb - g.ka) + BNK - 1) / BNK;
   per_head += (size_t)((d->T_k - p.k_pad) + BNK - 1) / BNK;
   const size_t fills =
@@ -886,10 +980,11 @@ size_t key_item_count(const sp_attn_desc* d, const Problem& p, int BNK) {
 }
 
 // Worst-case item counts (with empty items) for sizing.
-void item_counts(const sp_attn_desc* d, const Problem& p, int op, size_t& a, size_t& b) {
+void item_counts(const sp_attn_desc* d, const Problem& p, int op, const std::vector<spk::KeyCut>& cuts, size_t& a,
+                 size_t& b) {
   if (op == SP_OP_BWD) {
     a = row_item_count(d, p, spk::kDqBM);
-    b = key_item_count(d, p, spk::kDkdvBN);
+    b = key_item_count(d, p, cuts, spk::kDkdvBN);
   } else {
     a = row_item_count(d, p, spk::kFwdBM);
     b = 0;
@@ -1285,8 +1380,9 @@ sp_status sp_attn_workspace_size(const sp_attn_desc* desc, int32_t op, size_t* b
   if (s != SP_OK) return s;
   if (op == SP_OP_RING_STEP && !p.prefix.empty()) return SP_ERR_UNSUPPORTED;
   size_t a = 0, b = 0;
-  item_counts(desc, p, op, a, b);
-  *bytes = layout_for(desc, p, op, a, b).total;
+  const std::vector<spk::KeyCut> cuts = op == SP_OP_BWD ? key_cuts(desc, p) : std::vector<spk::KeyCut>();
+  item_counts(desc, p, op, cuts, a, b);
+  *bytes = layout_for(desc, p, op, a, b, cut_rows(p, cuts)).total;
   if (op == SP_OP_FWD) {  // (either way of a shared-prefix forward fits)
     const FewPlan f = few_plan(desc, p);
     if (f.parts) *bytes = std::max(*bytes, layout_few(desc, p, f).total);
@@ -1322,7 +1418,7 @@ sp_status sp_attn_schedule(const sp_attn_desc* desc, int32_t op, int32_t* items,
     schedule_rows(desc, p, spk::kFwdBM, spk::kFwdBN, true, v,
                   row_fills(desc, p).size() / kItemInts);
   else if (op == SP_OP_BWD)
-    schedule_keys(desc, p, spk::kDkdvBN, spk::kDkdvBQ, v, key_fills(desc, p).size() / kItemInts, items_);
+    schedule_keys(desc, p, spk::kDkdvBN, spk::kDkdvBQ, {}, v, key_fills(desc, p).size() / kItemInts, items_);
   else
     return SP_ERR_INVALID_ARG;
   const int32_t n = (int32_t)(v.size() / kItemInts);
@@ -1345,7 +1441,7 @@ sp_status sp_attn_plan(const sp_attn_desc* desc, int32_t op, int32_t* plan) {
   if (op == SP_OP_BWD) {
     std::vector<Item> keys;
     const Costs q = schedule_row_items(desc, p, tiles, spk::kDqBM, spk::kDqBN, true, v, 0, rows);
-    const Costs k = schedule_keys(desc, p, spk::kDkdvBN, spk::kDkdvBQ, v, 0, keys);
+    const Costs k = schedule_keys(desc, p, spk::kDkdvBN, spk::kDkdvBQ, key_cuts(desc, p), v, 0, keys);
     b = plan_bwd(q, k, p.D);
   } else {
     double us;
@@ -1561,13 +1657,14 @@ sp_status sp_attn_bwd(const sp_attn_desc* d, const void* q, const void* k, const
   const Costs cost_q =
       schedule_row_items(d, p, tiles, spk::kDqBM, spk::kDqBN, true, it_dq, fq.size() / kItemInts, rows);
   prepend(fq, it_dq);
+  const std::vector<spk::KeyCut> cuts = key_cuts(d, p);
   const Costs cost_k =
-      schedule_keys(d, p, spk::kDkdvBN, spk::kDkdvBQ, it_kv, fkv.size() / kItemInts, keys);
+      schedule_keys(d, p, spk::kDkdvBN, spk::kDkdvBQ, cuts, it_kv, fkv.size() / kItemInts, keys);
   prepend(fkv, it_kv);
   const size_t na = it_dq.size() / kItemInts, nb = it_kv.size() / kItemInts;
   // (the records of row tiles lie behind the dQ items, or in a launch's own list
   // behind all items)
-  Layout L = layout_for(d, p, SP_OP_BWD, na + record_room(tiles.size()) / kItemInts, nb);
+  Layout L = layout_for(d, p, SP_OP_BWD, na + record_room(tiles.size()) / kItemInts, nb, cut_rows(p, cuts));
   if ((s = check_ws(L, ws, ws_bytes)) != SP_OK) return s;
   hipStream_t st = (hipStream_t)stream;
   if ((s = refuse_capture(st)) != SP_OK) return s;
@@ -1629,6 +1726,8 @@ sp_status sp_attn_bwd(const sp_attn_desc* d, const void* q, const void* k, const
     b.dk = (uint16_t*)dk; b.dv = (uint16_t*)dv;
     b.part_k = p.direct ? nullptr : (float*)at(ws, L.part_k);
     b.part_v = p.direct ? nullptr : (float*)at(ws, L.part_v);
+    b.cut_k = cuts.empty() ? nullptr : (float*)at(ws, L.cut_k);
+    b.cut_v = cuts.empty() ? nullptr : (float*)at(ws, L.cut_v);
     b.items = by_value ? nullptr : (const int32_t*)at(ws, L.items_kv);
     b.T_q = d->T_q; b.T_k = d->T_k; b.H = d->H_loc; b.Hkv = d->Hkv_loc;
     b.scale_log2 = sl2; b.scale = d->softmax_scale; b.causal = d->causal; b.direct = p.direct;
@@ -1641,16 +1740,21 @@ sp_status sp_attn_bwd(const sp_attn_desc* d, const void* q, const void* k, const
     } else {
       SP_HIP(spk::launch_attn_dq(a, list, plan.q, D, prefix, st));
       if (by_value) std::copy(it_kv.begin(), it_kv.end(), list.v);
-      SP_HIP(spk::launch_attn_dkdv(b, list, plan.k, D, st));
+      SP_HIP(spk::launch_attn_dkdv(b, list, plan.k, D, prefix, st));
     }
-    if (!p.direct && p.n_real > 0) {
-      spk::ReduceArgs r{};
-      r.T = d->T_k; r.Hkv = d->Hkv_loc; r.D = D;
-      for (int kv = 0; kv < d->Hkv_loc; ++kv) {
-        r.head_lo[kv] = p.kv_lo[kv];
-        r.head_hi[kv] = p.kv_hi[kv];
-      }
-      SP_HIP(spk::launch_reduce_kv(b.part_k, b.part_v, dk, dv, r, st));
+    spk::CutArgs c{};
+    spk::ReduceArgs& r = c.r;
+    r.T = d->T_k; r.Hkv = d->Hkv_loc; r.D = D;
+    for (int kv = 0; kv < d->Hkv_loc; ++kv) {
+      r.head_lo[kv] = p.kv_lo[kv];
+      r.head_hi[kv] = p.kv_hi[kv];
+    }
+    if (!p.direct && p.n_real > 0) SP_HIP(spk::launch_reduce_kv(b.part_k, b.part_v, dk, dv, r, st));
+    if (!cuts.empty()) {
+      c.n_real = p.n_real;
+      c.n = (int)cuts.size();
+      std::copy(cuts.begin(), cuts.end(), c.c);
+      SP_HIP(spk::launch_cut_join(b.cut_k, b.cut_v, dk, dv, c, st));
     }
   }
   return SP_OK;

@@ -409,7 +409,9 @@ struct DkdvStage {
 // sequence, D = 128, RG = 1 / 2: 1024 rows 33 / 24 us, 4096 rows 102 / 68,
 // 16384 rows 480 / 587 us): pair p owns keys k0 + 32 (p % (NPF / RG)) ..
 // +32 and row group p / (NPF / RG), the chunks c with c % RG == its row group.
-template <int D, bool PWAVE, int RG, bool TWO>
+// CUT: the item may be a part of a shared prefix's (its last int then says where the
+// part's sums go).
+template <int D, bool PWAVE, int RG, bool TWO, bool CUT>
 SP_DEV void dkdv_body(const DkdvArgs& a, const int32_t (&it)[kItemInts], u32x4* smem, int w,
                       int lane) {
   using S = DkdvStage<D, TWO>;
@@ -643,7 +645,10 @@ SP_DEV void dkdv_body(const DkdvArgs& a, const int32_t (&it)[kItemInts], u32x4* 
     const int dim = (qi >> 2) * 32 + (qi & 3) * 8 + hh * 4;
     const float x0 = sum[i][0] * sc, x1 = sum[i][1] * sc;
     const float x2 = sum[i][2] * sc, x3 = sum[i][3] * sc;
-    if (a.direct) {
+    if (CUT && it[7] > kItemFillKV) {
+      const int64_t o = ((int64_t)((it[7] >> 2) - 1) + (key - k0)) * D + dim;
+      *(float4*)((PWAVE ? a.cut_v : a.cut_k) + o) = make_float4(x0, x1, x2, x3);
+    } else if (a.direct) {
       const int64_t o = ((int64_t)key * a.Hkv + kvh) * D + dim;
       *(u32x2*)((PWAVE ? a.dv : a.dk) + o) = pack_bf16x4(x0, x1, x2, x3);
     } else {
@@ -655,7 +660,7 @@ SP_DEV void dkdv_body(const DkdvArgs& a, const int32_t (&it)[kItemInts], u32x4* 
 
 // `block`: the workgroup's number among the launch's dK/dV workgroups; `base`:
 // the first dK/dV item in the list.
-template <int D, int RG, bool TWO>
+template <int D, int RG, bool TWO, bool CUT>
 SP_DEV void dkdv_wg(const DkdvArgs& a, const ItemList& list, int base, u32x4* smem, int block) {
   int32_t it[kItemInts];
   int pos, sub;
@@ -663,8 +668,10 @@ SP_DEV void dkdv_wg(const DkdvArgs& a, const ItemList& list, int base, u32x4* sm
   load_item(a.items, list, base, pos, it);
   if constexpr (RG > 1) {
     // (the first keys, which a causal mask shows to the most rows, first)
+    const int first = it[0];
     if (!split_rows<RG>(it[7] == kItemFillKV, 32 * NPF / RG, RG - 1 - sub, it[0], it[1])) return;
     if (a.causal) it[2] = max(it[2], it[0] - it[4]);
+    if (CUT && it[7] > kItemFillKV) it[7] += (it[0] - first) << 2;
   }
   if (it[7] == kItemFillKV) {  // KV head no real query head reads: dK = dV = +0
     fill_rows_bf16(a.dk, it[0], it[1], a.Hkv, it[6], D, threadIdx.x, 64 * 2 * NPF);
@@ -674,16 +681,16 @@ SP_DEV void dkdv_wg(const DkdvArgs& a, const ItemList& list, int base, u32x4* sm
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lane = threadIdx.x & 63;
   if (w < NPF)
-    dkdv_body<D, true, RG, TWO>(a, it, smem, w, lane);
+    dkdv_body<D, true, RG, TWO, CUT>(a, it, smem, w, lane);
   else
-    dkdv_body<D, false, RG, TWO>(a, it, smem, w, lane);
+    dkdv_body<D, false, RG, TWO, CUT>(a, it, smem, w, lane);
 }
 
-template <int D, int RG, bool TWO>
+template <int D, int RG, bool TWO, bool CUT>
 __global__ __launch_bounds__(64 * 2 * NPF, TWO ? 4 : 1) void attn_dkdv_kernel(DkdvArgs a,
                                                                              ItemList list) {
   __shared__ u32x4 smem[DkdvStage<D, TWO>::SMEM];
-  dkdv_wg<D, RG, TWO>(a, list, 0, smem, blockIdx.x);
+  dkdv_wg<D, RG, TWO, CUT>(a, list, 0, smem, blockIdx.x);
 }
 
 // -------------------------------------------------- dQ and dK / dV together
@@ -708,7 +715,7 @@ __global__ __launch_bounds__(NTQ, TWO ? 4 : 1) void attn_bwd_kernel(DqArgs a, Dk
       if (kind == 0 || kind == kItemFillQ)
         dq_body<D, KW, TWO, PFX>(a, list, smem, blockIdx.x);
       else
-        dkdv_wg<D, RG, TWO>(b, list, 0, smem, blockIdx.x);
+        dkdv_wg<D, RG, TWO, PFX>(b, list, 0, smem, blockIdx.x);
       return;
     }
   }
@@ -717,7 +724,7 @@ __global__ __launch_bounds__(NTQ, TWO ? 4 : 1) void attn_bwd_kernel(DqArgs a, Dk
   if (first == (dq_first != 0))
     dq_body<D, KW, TWO, PFX>(a, list, smem, block);
   else
-    dkdv_wg<D, RG, TWO>(b, list, a.n_items, smem, block);
+    dkdv_wg<D, RG, TWO, PFX>(b, list, a.n_items, smem, block);
 }
 
 }  // namespace
@@ -743,20 +750,20 @@ hipError_t launch_attn_dq(const DqArgs& a, const ItemList& list, LaunchShape s, 
 }
 
 template <int D, int RG, bool TWO>
-static hipError_t launch_dkdv(const DkdvArgs& a, const ItemList& list, hipStream_t st) {
-  return sp_launch(kKDkdv, attn_dkdv_kernel<D, RG, TWO>, dim3(split_grid(a.n_items, RG)),
+static hipError_t launch_dkdv(const DkdvArgs& a, const ItemList& list, bool prefix, hipStream_t st) {
+  return sp_launch(kKDkdv, prefix ? attn_dkdv_kernel<D, RG, TWO, true> : attn_dkdv_kernel<D, RG, TWO, false>, dim3(split_grid(a.n_items, RG)),
                    dim3(64 * 2 * NPF), st, a, list);
 }
 
-hipError_t launch_attn_dkdv(const DkdvArgs& a, const ItemList& list, LaunchShape s, int D,
+hipError_t launch_attn_dkdv(const DkdvArgs& a, const ItemList& list, LaunchShape s, int D, bool prefix,
                             hipStream_t st) {
   if (a.n_items <= 0) return hipSuccess;
   if (D == 128)
-    return s.split == 2 ? launch_dkdv<128, 2, false>(a, list, st)
-                        : launch_dkdv<128, 1, false>(a, list, st);
-  if (s.split == 2) return launch_dkdv<64, 2, false>(a, list, st);
-  if (s.two) return launch_dkdv<64, 1, true>(a, list, st);
-  return launch_dkdv<64, 1, false>(a, list, st);
+    return s.split == 2 ? launch_dkdv<128, 2, false>(a, list, prefix, st)
+                        : launch_dkdv<128, 1, false>(a, list, prefix, st);
+  if (s.split == 2) return launch_dkdv<64, 2, false>(a, list, prefix, st);
+  if (s.two) return launch_dkdv<64, 1, true>(a, list, prefix, st);
+  return launch_dkdv<64, 1, false>(a, list, prefix, st);
 }
 
 template <int D, int KW, int RG, bool TWO>

@@ -509,4 +509,36 @@ hipError_t launch_reduce_kv(const float* part_k, const float* part_v, void* dk, 
   return hipGetLastError();
 }
 
+// Blocks of gridDim.y cuts, y = 0, 1 of gridDim.z for dk and dv: one thread for eight
+// dims of a key and KV head, its parts and heads in a fixed order.
+__global__ __launch_bounds__(kBlock) void cut_join_kernel(const float* __restrict__ cut_k,
+                                                          const float* __restrict__ cut_v, uint16_t* __restrict__ dk,
+                                                          uint16_t* __restrict__ dv, CutArgs a) {
+  const KeyCut cut = a.c[blockIdx.y];
+  const int n8 = a.r.D >> 3, Hkv = a.r.Hkv;
+  const int64_t e = (int64_t)blockIdx.x * kBlock + threadIdx.x;
+  if (e >= (int64_t)cut.len * Hkv * n8) return;
+  const int c = (int)(e % n8), kv = (int)(e / n8 % Hkv), t = (int)(e / n8 / Hkv);
+  const float* in = (blockIdx.z ? cut_v : cut_k) + ((int64_t)cut.row + t) * a.r.D + c * 8;
+  float s[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+  for (int y = a.r.head_lo[kv]; y < a.r.head_hi[kv]; ++y)
+#pragma unroll 4
+    for (int i = 0; i < cut.parts; ++i) {
+      const float4* p = (const float4*)(in + ((int64_t)i * a.n_real + y) * cut.len * a.r.D);
+      const float4 u = p[0], w = p[1];
+      s[0] += u.x; s[1] += u.y; s[2] += u.z; s[3] += u.w;
+      s[4] += w.x; s[5] += w.y; s[6] += w.z; s[7] += w.w;
+    }
+  *(u32x4*)((blockIdx.z ? dv : dk) + (((int64_t)cut.ka + t) * Hkv + kv) * a.r.D + c * 8) =
+      pack_bf16x8(s[0], s[1], s[2], s[3], s[4], s[5], s[6], s[7]);
+}
+
+hipError_t launch_cut_join(const float* cut_k, const float* cut_v, void* dk, void* dv, const CutArgs& a, hipStream_t st) {
+  int64_t most = 0;
+  for (int i = 0; i < a.n; ++i) most = std::max<int64_t>(most, (int64_t)a.c[i].len * a.r.Hkv * (a.r.D / 8));
+  if (most == 0) return hipSuccess;
+  return sp_launch(0, cut_join_kernel, dim3((unsigned)((most + kBlock - 1) / kBlock), a.n, 2), dim3(kBlock), st, cut_k,
+                   cut_v, (uint16_t*)dk, (uint16_t*)dv, a);
+}
+
 }  // namespace spk

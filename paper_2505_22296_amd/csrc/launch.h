@@ -136,6 +136,8 @@ struct ReduceArgs {
 // Work item of the attention kernels: 8 int32.
 //   fwd / dq:  {q_begin, q_end, k_begin, k_end, delta, head, kv_head, 0}
 //   dk/dv:     {k_begin, k_end, q_begin, q_end, delta, head, kv_head, 1}
+//   the same of a shared prefix's keys whose rows are cut into parts (KeyCut):
+//              its last int is 1 | (1 + r) << 2, r the row of k_begin in cut_k, cut_v
 //   fwd / dq of a batch with shared prefixes:
 //              {record, 0, 0, 0, 0, head, kv_head, 0}: the record of the item's
 //              first workgroup, in ints from the list's start (layout: RowSlot)
@@ -176,6 +178,18 @@ struct FwdArgs {
   int parts;           // few rows: of every tile's keys
 };
 
+// Keys [ka, ka + len) of a shared prefix, whose rows' gradients are formed in `parts`
+// parts: part i of head y at rows row + (i * n_real + y) * len of cut_k, cut_v.
+struct KeyCut {
+  int ka, len, parts, row;
+};
+static constexpr int kMaxCuts = 32;  // of a call
+struct CutArgs {
+  ReduceArgs r;
+  int n_real, n;
+  KeyCut c[kMaxCuts];
+};
+
 struct DqArgs {
   const uint16_t* q;     // [T_q, H, D]
   const uint16_t* k;     // [T_k, Hkv, D]
@@ -205,6 +219,8 @@ struct DkdvArgs {
   uint16_t* dv;
   float* part_k;         // float32 [n_real, T_k, D] (GQA partial mode)
   float* part_v;
+  float* cut_k;          // float32 [rows, D]: parts of cut items (KeyCut)
+  float* cut_v;
   const int32_t* items;  // null: in the launch's ItemList
   int T_q, T_k, H, Hkv;
   float scale_log2, scale;
@@ -248,6 +264,8 @@ hipError_t launch_fill_f32(float* x, int64_t n, float v, hipStream_t st);
 hipError_t launch_f32_to_bf16(const float* s, void* d, int64_t n, hipStream_t st);
 hipError_t launch_rowdot(const void* o, const void* dout, const float* lse, float* neg_d,
                          float* lse2, int T, int H, int nh, int D, hipStream_t st);
+// Sums of the parts and heads of cut keys, over whatever else wrote their dk, dv.
+hipError_t launch_cut_join(const float* cut_k, const float* cut_v, void* dk, void* dv, const CutArgs& a, hipStream_t st);
 hipError_t launch_reduce_kv(const float* part_k, const float* part_v, void* dk, void* dv,
                             const ReduceArgs& a, hipStream_t st);
 
@@ -277,7 +295,7 @@ static constexpr int few_steps(int k0, int k1, int tile_keys) {  // key tiles of
 static constexpr int kMaxParts = 256;
 hipError_t launch_attn_few(const FwdArgs& a, const ItemList& list, int D, int n_real, hipStream_t st);
 hipError_t launch_attn_dq(const DqArgs& a, const ItemList& list, LaunchShape s, int D, bool prefix, hipStream_t st);
-hipError_t launch_attn_dkdv(const DkdvArgs& a, const ItemList& list, LaunchShape s, int D, hipStream_t st);
+hipError_t launch_attn_dkdv(const DkdvArgs& a, const ItemList& list, LaunchShape s, int D, bool prefix, hipStream_t st);
 // dQ and dK/dV in one launch; (q.split, k.split) one of (4, 2), (2, 1),
 // (1, 1); two workgroups a CU for (1, 1) alone, q.two.  `dq_first`: the dQ workgroups
 // come first; `merged` (with `prefix`, for (1, 1)): both kinds are in one list, a's,

@@ -306,3 +306,44 @@ def test_prefix_offsets_past_32_bits(sp):
             assert (a.float() - b.float()).abs().max() <= 8 * STEP16 * b.float().abs().max()
         assert not dk[:n].any() and not dv[:n].any()
         del K, V, dk, dv
+
+
+MANY = [  # rows (and keys) of the groups, prefixes, query and KV heads, dummies, D, causal
+    ([130] + [300] * 6, [-1] + [0] * 6, 1, 1, 0, 128, True),
+    ([40] + [217] * 9, [-1] + [0] * 9, 4, 2, 0, 64, True),           # one tile of keys
+    ([301, 1, 0] + [300] * 13, [-1] + [0] * 15, 3, 3, 1, 64, True),   # an odd last tile, a dummy
+    ([70, 800, 400, 900, 33, 700, 9, 1100], [-1, 0, 0, 0, -1, 4, 4, 4], 2, 1, 0, 128, True),  # two groups
+    ([129, 513, 640, 511], [-1, 0, 0, 0], 2, 1, 0, 128, False),
+    ([64, 600] + [310] * 16, [-1] + [0] * 17, 7, 1, 0, 64, True),
+    ([0, 2500, 1900], [-1, 0, 0], 2, 2, 0, 128, True),                 # the prefix's keys alone
+    ([130] + [20] * 200, [-1] + [0] * 200, 4, 1, 0, 128, True),       # both kinds of items in one list
+    ([70] + [33] * 150, [-1] + [0] * 150, 7, 1, 0, 64, True),         # and two workgroups a CU
+]
+
+
+@pytest.mark.parametrize("nq,pre,hq,hkv,dummies,D,causal", MANY)
+def test_prefix_of_many_rows(sp, nq, pre, hq, hkv, dummies, D, causal):
+    """A short prompt, whose few key tiles see every answer's rows: those are cut into
+    parts, and their sums joined."""
+    nk = [n if n or i else 200 for i, n in enumerate(nq)]
+    d, p = desc(nq, nk, pre, D=D, hq=hq, hkv=hkv, dummies=dummies, causal=causal, pad_k=5 if D == 64 else 0)
+    alone, _ = desc(nq, nk, [-1] * len(nq), D=D, hq=hq, hkv=hkv, dummies=dummies, causal=causal, pad_k=5 if D == 64 else 0)
+    sizes = [sp.sp_attn_workspace_size(x, sp.SP_OP_BWD) for x in (d, alone)]
+    assert sizes[0] - sizes[1] >= 1.5 * 2 * nk[0] * hq * D * 4  # (two parts at least, and fewer items)
+    o, lse, dq, dk, dv = compare(sp, d, p, seed=len(nq))
+    # over K and V, in two launches
+    q, k, v, do = inputs(d, len(nq))
+    sp.sp_attn_bwd(d, q, k, v, o, lse, do, dk=k, dv=v)
+    assert torch.equal(k, dk) and torch.equal(v, dv)
+
+
+def test_prefix_of_many_rows_over_a_spoiled_workspace(sp):
+    """Parts without rows are written too: nothing of the workspace's old content shows."""
+    nq, pre = [257, 2600, 1, 2000], [-1, 0, 0, 0]
+    d, _ = desc(nq, nq, pre, D=64, hq=2, hkv=2)
+    q, k, v, do = inputs(d, 8)
+    o, lse = sp.sp_attn_fwd(d, q, k, v)
+    n = sp.sp_attn_workspace_size(d, sp.SP_OP_BWD)
+    grads = [sp.sp_attn_bwd(d, q, k, v, o, lse, do, workspace=torch.full((n,), x, dtype=torch.uint8, device="cuda"))
+             for x in (0, 255)]
+    assert all(torch.equal(a, b) for a, b in zip(*grads))
