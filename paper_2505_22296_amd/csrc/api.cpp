@@ -743,9 +743,9 @@ Costs schedule_keys(const sp_attn_desc* d, const Problem& p, int BNK, int BQ, co
         if (d->causal) q0 = (int)std::max<int64_t>(g.qa, (int64_t)a - g.delta);
         const bool empty = q0 >= g.qb;
         if (cut) {  // (parts without rows write zeros)
-          const int n = std::max(0, g.qb - q0), rows = ((n + cut->parts - 1) / cut->parts + BQ - 1) / BQ * BQ;
+          const int64_t n = std::max(0, g.qb - q0), rows = ((n + cut->parts - 1) / cut->parts + BQ - 1) / BQ * BQ;
           for (int i = 0; i < cut->parts; ++i) {
-            const int r0 = g.qb - std::min(n, i * rows), r1 = g.qb - std::min<int64_t>(n, (int64_t)(i + 1) * rows);
+            const int r0 = (int)(g.qb - std::min(n, i * rows)), r1 = (int)(g.qb - std::min(n, (i + 1) * rows));
             const int at = cut->row + (i * p.n_real + y) * cut->len + (a - g.ka);
             items.push_back(Item{{a, b, r1, r0, g.delta, y, p.kv_of[y], 1 | (1 + at) << 2},
                                  r1 < r0 ? ((r0 - (r1 & ~7)) + BQ - 1) / BQ : 0});
@@ -1740,7 +1740,7 @@ sp_status sp_attn_bwd(const sp_attn_desc* d, const void* q, const void* k, const
     } else {
       SP_HIP(spk::launch_attn_dq(a, list, plan.q, D, prefix, st));
       if (by_value) std::copy(it_kv.begin(), it_kv.end(), list.v);
-      SP_HIP(spk::launch_attn_dkdv(b, list, plan.k, D, prefix, st));
+      SP_HIP(spk::launch_attn_dkdv(b, list, plan.k, D, st));
     }
     spk::CutArgs c{};
     spk::ReduceArgs& r = c.r;

@@ -702,7 +702,9 @@ __global__ __launch_bounds__(64 * 2 * NPF, TWO ? 4 : 1) void attn_dkdv_kernel(Dk
 // mask 245 / 193).  Workgroups
 // [0, n_first) run the list with the longer workgroups: 28 heads of 2048 rows
 // 148 us with dQ, whose items are the longer ones there, first, 160 us last.
-template <int D, int KW, int RG, bool TWO, bool PFX>
+// CUT (with PFX): the list has parts of items.  (A kernel of its own: the branch costs
+// lists without them 0.8%, 780 to 786 us for 16 answers of 660 rows to 7675 keys.)
+template <int D, int KW, int RG, bool TWO, bool PFX, bool CUT>
 __global__ __launch_bounds__(NTQ, TWO ? 4 : 1) void attn_bwd_kernel(DqArgs a, DkdvArgs b, ItemList list,
                                                           int n_first, int dq_first) {
   static_assert(NTQ == 64 * 2 * NPF, "one workgroup size");
@@ -715,7 +717,7 @@ __global__ __launch_bounds__(NTQ, TWO ? 4 : 1) void attn_bwd_kernel(DqArgs a, Dk
       if (kind == 0 || kind == kItemFillQ)
         dq_body<D, KW, TWO, PFX>(a, list, smem, blockIdx.x);
       else
-        dkdv_wg<D, RG, TWO, PFX>(b, list, 0, smem, blockIdx.x);
+        dkdv_wg<D, RG, TWO, CUT>(b, list, 0, smem, blockIdx.x);
       return;
     }
   }
@@ -724,7 +726,7 @@ __global__ __launch_bounds__(NTQ, TWO ? 4 : 1) void attn_bwd_kernel(DqArgs a, Dk
   if (first == (dq_first != 0))
     dq_body<D, KW, TWO, PFX>(a, list, smem, block);
   else
-    dkdv_wg<D, RG, TWO, PFX>(b, list, a.n_items, smem, block);
+    dkdv_wg<D, RG, TWO, CUT>(b, list, a.n_items, smem, block);
 }
 
 }  // namespace
@@ -750,20 +752,20 @@ hipError_t launch_attn_dq(const DqArgs& a, const ItemList& list, LaunchShape s, 
 }
 
 template <int D, int RG, bool TWO>
-static hipError_t launch_dkdv(const DkdvArgs& a, const ItemList& list, bool prefix, hipStream_t st) {
-  return sp_launch(kKDkdv, prefix ? attn_dkdv_kernel<D, RG, TWO, true> : attn_dkdv_kernel<D, RG, TWO, false>, dim3(split_grid(a.n_items, RG)),
+static hipError_t launch_dkdv(const DkdvArgs& a, const ItemList& list, hipStream_t st) {
+  return sp_launch(kKDkdv, a.cut_k ? attn_dkdv_kernel<D, RG, TWO, true> : attn_dkdv_kernel<D, RG, TWO, false>, dim3(split_grid(a.n_items, RG)),
                    dim3(64 * 2 * NPF), st, a, list);
 }
 
-hipError_t launch_attn_dkdv(const DkdvArgs& a, const ItemList& list, LaunchShape s, int D, bool prefix,
+hipError_t launch_attn_dkdv(const DkdvArgs& a, const ItemList& list, LaunchShape s, int D,
                             hipStream_t st) {
   if (a.n_items <= 0) return hipSuccess;
   if (D == 128)
-    return s.split == 2 ? launch_dkdv<128, 2, false>(a, list, prefix, st)
-                        : launch_dkdv<128, 1, false>(a, list, prefix, st);
-  if (s.split == 2) return launch_dkdv<64, 2, false>(a, list, prefix, st);
-  if (s.two) return launch_dkdv<64, 1, true>(a, list, prefix, st);
-  return launch_dkdv<64, 1, false>(a, list, prefix, st);
+    return s.split == 2 ? launch_dkdv<128, 2, false>(a, list, st)
+                        : launch_dkdv<128, 1, false>(a, list, st);
+  if (s.split == 2) return launch_dkdv<64, 2, false>(a, list, st);
+  if (s.two) return launch_dkdv<64, 1, true>(a, list, st);
+  return launch_dkdv<64, 1, false>(a, list, st);
 }
 
 template <int D, int KW, int RG, bool TWO>
@@ -771,16 +773,19 @@ static hipError_t launch_bwd(const DqArgs& a, const DkdvArgs& b, const ItemList&
                              bool dq_first, bool prefix, bool merged, hipStream_t st) {
   if (merged) {
     if (!prefix || KW != 1 || RG != 1) return hipErrorInvalidValue;
-    return sp_launch2(kKDq, kKDkdv, attn_bwd_kernel<D, KW, RG, TWO, true>, dim3(a.n_items), dim3(NTQ), st, a, b, list,
-                      -1, 0);
+    return sp_launch2(kKDq, kKDkdv,
+                      b.cut_k ? attn_bwd_kernel<D, KW, RG, TWO, true, true> : attn_bwd_kernel<D, KW, RG, TWO, true, false>,
+                      dim3(a.n_items), dim3(NTQ), st, a, b, list, -1, 0);
   }
   // the first list's workgroups are rounded up to eight, so that the second
   // list's positions keep their XCDs
   const int nq = split_grid(a.n_items, KW), nk = split_grid(b.n_items, RG);
   const int n_first = ((dq_first ? nq : nk) + 7) / 8 * 8;
   const dim3 grid(n_first + (dq_first ? nk : nq)), block(NTQ);
-  return sp_launch2(kKDq, kKDkdv, prefix ? attn_bwd_kernel<D, KW, RG, TWO, true> : attn_bwd_kernel<D, KW, RG, TWO, false>,
-                    grid, block, st, a, b, list, n_first, (int)dq_first);
+  auto* kernel = b.cut_k  ? attn_bwd_kernel<D, KW, RG, TWO, true, true>
+                 : prefix ? attn_bwd_kernel<D, KW, RG, TWO, true, false>
+                          : attn_bwd_kernel<D, KW, RG, TWO, false, false>;
+  return sp_launch2(kKDq, kKDkdv, kernel, grid, block, st, a, b, list, n_first, (int)dq_first);
 }
 
 hipError_t launch_attn_bwd(const DqArgs& a, const DkdvArgs& b, const ItemList& list, LaunchShape q,

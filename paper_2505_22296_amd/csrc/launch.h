@@ -295,7 +295,7 @@ static constexpr int few_steps(int k0, int k1, int tile_keys) {  // key tiles of
 static constexpr int kMaxParts = 256;
 hipError_t launch_attn_few(const FwdArgs& a, const ItemList& list, int D, int n_real, hipStream_t st);
 hipError_t launch_attn_dq(const DqArgs& a, const ItemList& list, LaunchShape s, int D, bool prefix, hipStream_t st);
-hipError_t launch_attn_dkdv(const DkdvArgs& a, const ItemList& list, LaunchShape s, int D, bool prefix, hipStream_t st);
+hipError_t launch_attn_dkdv(const DkdvArgs& a, const ItemList& list, LaunchShape s, int D, hipStream_t st);
 // dQ and dK/dV in one launch; (q.split, k.split) one of (4, 2), (2, 1),
 // (1, 1); two workgroups a CU for (1, 1) alone, q.two.  `dq_first`: the dQ workgroups
 // come first; `merged` (with `prefix`, for (1, 1)): both kinds are in one list, a's,
